@@ -276,6 +276,114 @@ vc_status vc_attn_forward_codes(const vc_shape *shape, const vc_opts *opts, cons
 vc_status vc_fp8_score_product(const uint8_t *a, const uint8_t *bm, const float *c_in, float *out, int32_t n,
                                void *stream);
 
+/* ---- Operators around the attention of a block ---------------------------------------------------
+ *
+ * What a video transformer's block does next to the attention above: the norms of queries and keys with
+ * the rotation by position, and the attention to the states of another sequence. Their tensors are bf16
+ * or fp16, addressed by strides, so that they are read from packed projections ([B, N, heads, d] parts
+ * of a wider row) and written in the order that the next step reads. The conventions at the top hold,
+ * but for the contiguity of the tensors passed as views. */
+
+enum { VC_BF16 = 0, VC_FP16 = 1 };
+
+/* A 16-bit tensor [B, heads, rows, d] in device memory: element (b, h, n, c) stands at
+ * data[b * sb + h * sh + n * sn + c]; the channels of a row are contiguous. data is 16-byte aligned and the
+ * strides are multiples of 8 elements (VC_ERR_ALIGN otherwise), not negative, and (extent - 1) * stride is at most
+ * 2^40 elements (VC_ERR_SHAPE). The stride of an axis of extent 1 is not used. An input may have strides of 0 (a
+ * tensor shared along an axis); the rows of an output must be distinct: sorted by stride, each axis' stride is at
+ * least the span of those before it (VC_ERR_SHAPE otherwise). */
+typedef struct {
+    void *data;
+    int64_t sb, sh, sn;
+} vc_view;
+
+enum { VC_NORM_NONE = 0,    /* the rotation alone */
+       VC_NORM_HEAD = 1,    /* each row of d channels on its own, weights [d] shared by the heads */
+       VC_NORM_TOKEN = 2 }; /* all heads of a token together, weights [heads * d] */
+enum { VC_ROPE_NONE = 0,        /* the norm alone */
+       VC_ROPE_INTERLEAVED = 1, /* pair i turns channels 2i and 2i + 1 */
+       VC_ROPE_HALF = 2 };      /* pair i turns channels i and rot/2 + i */
+
+/* Shape of the norm and rotation: B sequences of N tokens, Hq query heads and Hk key heads of d = 64 or 128
+ * channels; B, N, Hq >= 1, Hk >= 0 (0: queries only), B * N < 2^31, (Hq + Hk) * d <= 2^20, and for VC_NORM_TOKEN
+ * Hq * d and Hk * d at most 8192 (VC_ERR_SHAPE otherwise). */
+typedef struct {
+    int32_t B, Hq, Hk, N, d;
+} vc_norm_rope_shape;
+
+/* Options of the norm and rotation.
+ *   dtype  : VC_BF16 or VC_FP16, of all tensors. Sums, norms and angles are fp32, outputs are rounded once.
+ *   norm   : as above; y = x / sqrt(mean(x^2) + eps) * weight. The sum of squares under one norm must be finite in
+ *            fp32 (a bf16 row beyond that comes out as 0, or NaN where an element is not finite).
+ *   layout : as above. With VC_ROPE_NONE, norm must not be VC_NORM_NONE.
+ *   rot    : channels that are turned, the first `rot` of each head: a multiple of 16, 16 <= rot <= d (0 with
+ *            VC_ROPE_NONE). The others pass (normed) as they are.
+ *   eps    : > 0 and finite where there is a norm.
+ *   rows   : rows of the tables for positions on a line (F = 0): [rows, rot/2] fp32, row p the cos / sin of
+ *            position p (vc_rope_line_tables). rows >= 1.
+ *   F, Ht, Wd : all 0 (a line), or a latent grid with F * Ht * Wd = N: token n turns by its frame, row and column with
+ *            the tables of vc_rope_tables ([F + Ht + Wd, 64]); d and rot must then be 128. `rows` is not used.
+ * VC_ERR_UNSUPPORTED for a value outside these. */
+typedef struct {
+    int32_t dtype, norm, layout, rot;
+    float eps;
+    int32_t rows;
+    int32_t F, Ht, Wd;
+} vc_norm_rope_opts;
+
+/* Norms of queries and keys and the rotation by position, in one pass.
+ *   q, k         : inputs [B, Hq, N, d] and [B, Hk, N, d] (k NULL when Hk = 0).
+ *   q_weight, k_weight : fp32 weights of the norms ([d], or [heads * d]); NULL: ones.
+ *   rope_cos, rope_sin : device tables (not read with VC_ROPE_NONE).
+ *   pos          : int32 [B, N], 4-byte aligned: each token's row of the tables (entries outside are clamped, the
+ *                  result is then unspecified); NULL: row n, for which rows >= N. NULL on a grid.
+ *   q_out, k_out : outputs; they may be the inputs themselves (the same view), not overlap otherwise. */
+vc_status vc_norm_rope(const vc_norm_rope_shape *shape, const vc_norm_rope_opts *opts, const vc_view *q,
+                       const vc_view *k, const float *q_weight, const float *k_weight, const float *rope_cos,
+                       const float *rope_sin, const int32_t *pos, const vc_view *q_out, const vc_view *k_out,
+                       void *stream);
+
+/* Bytes of device workspace that vc_norm_rope_backward needs (0 for VC_NORM_NONE). Returns (size_t)-1 if the
+ * shape or options are invalid. */
+size_t vc_norm_rope_workspace_size(const vc_norm_rope_shape *shape, const vc_norm_rope_opts *opts);
+
+/* Gradients of vc_norm_rope.
+ *   q, k, weights, tables, pos : as given to vc_norm_rope (q and k may be NULL with VC_NORM_NONE: the
+ *              rotation's gradient needs none of its input).
+ *   dq_out, dk_out : gradients of the outputs.
+ *   dq, dk         : gradients of the inputs, written; they may be dq_out / dk_out themselves.
+ *   dq_weight, dk_weight : fp32 gradients of the weights, written (not added to); NULL: not formed. They must be
+ *              NULL with VC_NORM_NONE. Their sums are formed in an order that depends on the shape alone.
+ *   ws         : device workspace of ws_bytes >= vc_norm_rope_workspace_size(shape, opts); may be NULL when neither
+ *              weight gradient is asked for. */
+vc_status vc_norm_rope_backward(const vc_norm_rope_shape *shape, const vc_norm_rope_opts *opts, const vc_view *q,
+                                const vc_view *k, const float *q_weight, const float *k_weight, const float *rope_cos,
+                                const float *rope_sin, const int32_t *pos, const vc_view *dq_out,
+                                const vc_view *dk_out, const vc_view *dq, const vc_view *dk, float *dq_weight,
+                                float *dk_weight, void *ws, size_t ws_bytes, void *stream);
+
+enum { VC_SCALE_NONE = 0,   /* angle pos * theta^(-2i / rot) of pair i */
+       VC_SCALE_LINEAR = 1, /* positions divided by `factor` */
+       VC_SCALE_BASE = 2,   /* theta raised to theta * factor^(rot / (rot - 2)): the last pair is slowed by `factor`, the
+                             * first stays */
+       VC_SCALE_PARTS = 3 };/* pairs that turn more than `fast` times over `trained` positions stay, those that turn less
+                             * than `slow` times are slowed by `factor`, linear in the turns between */
+
+/* Scaling of the angles for contexts `factor` (>= 1) times those of the training. trained, fast and slow are
+ * read for VC_SCALE_PARTS only (trained >= 1, fast > slow >= 0). magnitude multiplies cos and sin
+ * (0 selects 1): the attention's temperature at long contexts, e.g. 0.1 ln(factor) + 1. */
+typedef struct {
+    int32_t kind;
+    double factor, trained, fast, slow, magnitude;
+} vc_rope_scaling;
+
+/* HOST helper: rotary tables of positions 0 .. rows-1 on a line, written to host arrays cos_t/sin_t of rows x rot/2
+ * fp32. Angles are evaluated in fp64 and rounded once to fp32. scaling may be NULL (none). Returns VC_ERR_NULL on
+ * NULL tables, VC_ERR_SHAPE for rows < 1, a rot that is not a multiple of 16 in [16, 128], rows * rot / 2 >= 2^31 or
+ * a theta that is not finite and positive, VC_ERR_UNSUPPORTED for an invalid scaling. */
+vc_status vc_rope_line_tables(int32_t rows, int32_t rot, double theta, const vc_rope_scaling *scaling, float *cos_t,
+                              float *sin_t);
+
 /* Static description of a status code. */
 const char *vc_status_str(vc_status s);
 

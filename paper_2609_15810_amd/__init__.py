@@ -23,6 +23,10 @@ STATUS = {0: "VC_OK", 1: "VC_ERR_NULL", 2: "VC_ERR_SHAPE", 3: "VC_ERR_UNSUPPORTE
 P_EXPCAST, P_EXP_THEN_CAST = 0, 1
 QK_INT8, QK_FP8, QK_MXFP4 = 0, 1, 2
 GROUP_IDENTITY, GROUP_CUBE, GROUP_KMEANS = 0, 1, 2
+BF16, FP16 = 0, 1
+NORM_NONE, NORM_HEAD, NORM_TOKEN = 0, 1, 2
+ROPE_NONE, ROPE_INTERLEAVED, ROPE_HALF = 0, 1, 2
+SCALE_NONE, SCALE_LINEAR, SCALE_BASE, SCALE_PARTS = 0, 1, 2, 3
 
 
 class VcError(RuntimeError):
@@ -53,6 +57,23 @@ class GroupOpts(C.Structure):
 class Prepped(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("q", "q_scale", "k", "k_scale", "k_mean", "v", "v_scale", "v_mean",
                                           "q_mx_scale", "k_mx_scale")]
+
+
+class View(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("sb", C.c_int64), ("sh", C.c_int64), ("sn", C.c_int64)]
+
+
+class NormRopeShape(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("B", "Hq", "Hk", "N", "d")]
+
+
+class NormRopeOpts(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("norm", C.c_int32), ("layout", C.c_int32), ("rot", C.c_int32),
+                ("eps", C.c_float), ("rows", C.c_int32), ("F", C.c_int32), ("Ht", C.c_int32), ("Wd", C.c_int32)]
+
+
+class RopeScaling(C.Structure):
+    _fields_ = [("kind", C.c_int32)] + [(n, C.c_double) for n in ("factor", "trained", "fast", "slow", "magnitude")]
 
 
 _lib = None
@@ -92,6 +113,18 @@ def lib():
                                             C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
         L.vc_fp8_score_product.restype = C.c_int
         L.vc_fp8_score_product.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p]
+        L.vc_norm_rope.restype = C.c_int
+        L.vc_norm_rope.argtypes = [C.POINTER(NormRopeShape), C.POINTER(NormRopeOpts)] + [C.POINTER(View)] * 2 + \
+            [C.c_void_p] * 5 + [C.POINTER(View)] * 2 + [C.c_void_p]
+        L.vc_norm_rope_workspace_size.restype = C.c_size_t
+        L.vc_norm_rope_workspace_size.argtypes = [C.POINTER(NormRopeShape), C.POINTER(NormRopeOpts)]
+        L.vc_norm_rope_backward.restype = C.c_int
+        L.vc_norm_rope_backward.argtypes = [C.POINTER(NormRopeShape), C.POINTER(NormRopeOpts)] + \
+            [C.POINTER(View)] * 2 + [C.c_void_p] * 5 + [C.POINTER(View)] * 4 + \
+            [C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.vc_rope_line_tables.restype = C.c_int
+        L.vc_rope_line_tables.argtypes = [C.c_int32, C.c_int32, C.c_double, C.POINTER(RopeScaling), C.c_void_p,
+                                          C.c_void_p]
         L.vc_opts_default.argtypes = [C.POINTER(Opts)]
         L.vc_group_opts_default.argtypes = [C.POINTER(GroupOpts)]
         _lib = L
@@ -277,3 +310,142 @@ class Attention:
     def forward_codes(self, O, p_codes, q_perm=None, stream=None):
         """forward() that also writes the probability codes, uint8 [B, H, N, 128 T] (debugging)."""
         vc_attn_forward_codes(self.shape, self.opts, self.prepped, q_perm, O, p_codes, stream)
+
+
+# ---- operators around the attention --------------------------------------------------------------
+
+def make_rope_scaling(kind=SCALE_NONE, factor=1.0, trained=4096, fast=32.0, slow=1.0, magnitude=0.0) -> RopeScaling:
+    return RopeScaling(int(kind), float(factor), float(trained), float(fast), float(slow), float(magnitude))
+
+
+def rope_line_tables_host(rows: int, rot: int = D, theta: float = 10000.0, scaling: RopeScaling | None = None):
+    """vc_rope_line_tables into host numpy arrays [rows, rot/2] fp32."""
+    cos_t = np.empty((max(rows, 0), max(rot, 0) // 2), np.float32)
+    sin_t = np.empty_like(cos_t)
+    _check("vc_rope_line_tables", lib().vc_rope_line_tables(
+        rows, rot, float(theta), C.byref(scaling) if scaling is not None else None, cos_t.ctypes.data,
+        sin_t.ctypes.data))
+    return cos_t, sin_t
+
+
+class _Operands:
+    """Marshalling of one operator's tensors: checks each against its shape, type and device (the library sees
+    addresses only) and makes the C arguments. Raises VcError as the library would."""
+
+    def __init__(self, fn, dtype, device):
+        self.fn, self.dtype, self.device = fn, dtype, device
+
+    def refuse(self, status):
+        raise VcError(self.fn, status, lib())
+
+    def view(self, t, shape):
+        if t is None:
+            return None
+        if tuple(t.shape) != shape or t.dtype != self.dtype or t.device != self.device:
+            self.refuse(2)
+        sb, sh, sn, sc = t.stride()
+        if sc != 1:
+            self.refuse(5)
+        return C.byref(View(t.data_ptr(), sb, sh, sn))
+
+    def flat(self, t, shape, dtype):
+        """address of a contiguous tensor (shape None: of any)"""
+        if t is None:
+            return None
+        if (shape is not None and tuple(t.shape) != shape) or t.dtype != dtype or t.device != self.device:
+            self.refuse(2)
+        if not t.is_contiguous():
+            self.refuse(5)
+        return t.data_ptr()
+
+
+def _device(device):
+    import torch
+    d = torch.device(device)
+    return torch.device(d.type, torch.cuda.current_device()) if d.type == "cuda" and d.index is None else d
+
+
+class _Operator:
+    """What the operators around the attention have in common: a call runs on the device of its tensors, on the
+    given stream or that device's current one."""
+
+    def __init__(self, dtype, device):
+        import torch
+        types = {torch.bfloat16: BF16, torch.float16: FP16}
+        if dtype not in types:
+            raise VcError(type(self).__name__, 3, lib())
+        self.dtype, self.device = dtype, _device(device)
+        self.c_dtype = types[dtype]
+        self.ws = None
+
+    def _call(self, fn, stream, *args):
+        import torch
+        s = torch.cuda.current_stream(self.device) if stream is None else stream
+        L = getattr(lib(), fn)
+        if torch.cuda.current_device() == self.device.index:
+            st = L(*args, s.cuda_stream)
+        else:
+            with torch.cuda.device(self.device):
+                st = L(*args, s.cuda_stream)
+        _check(fn, st)
+
+
+class NormRope(_Operator):
+    """Norms of queries and keys with the rotation by position, for one shape: vc_norm_rope and its gradients.
+
+    Tensors are [B, heads, N, d] of `dtype` in any strides whose channels are contiguous (a transposed view of
+    a packed projection). grid: (frames, rows, columns) with the tables of vc_rope_tables; None: positions on a line
+    with [rows, rot/2] tables. training: hold the workspace of the weights' gradients. Two calls that overlap in
+    time (on two streams, or two captured graphs) need an object each: backward() uses the object's workspace.
+    """
+
+    def __init__(self, B, Hq, Hk, N, d=D, norm=NORM_HEAD, eps=1e-6, layout=ROPE_INTERLEAVED, rot=None, grid=None,
+                 dtype=None, training=False, device="cuda"):
+        import torch
+        super().__init__(torch.bfloat16 if dtype is None else dtype, device)
+        self.shape = NormRopeShape(B, Hq, Hk, N, d)
+        rot = 0 if layout == ROPE_NONE else (d if rot is None else rot)
+        # the tables' rows are known with the tables; 1 stands for them in the checks here
+        self.opts = NormRopeOpts(self.c_dtype, norm, layout, rot, eps, 1, *(grid or (0, 0, 0)))
+        size = lib().vc_norm_rope_workspace_size(C.byref(self.shape), C.byref(self.opts))
+        if size == C.c_size_t(-1).value:
+            raise VcError("vc_norm_rope_workspace_size", 2, lib())
+        if training:
+            self.ws = torch.empty(max(size, 16), dtype=torch.uint8, device=self.device)
+        self._sizes = (B, Hq, N, d), (B, Hk, N, d)
+
+    def _common(self, fn, q, k, q_weight, k_weight, cos, sin, pos):
+        import torch
+        x, (sq, sk), o = _Operands(fn, self.dtype, self.device), self._sizes, self.opts
+        if (k is not None or k_weight is not None) and sk[1] == 0:
+            x.refuse(2)
+        if o.layout != ROPE_NONE:
+            if cos is None or sin is None:
+                x.refuse(1)
+            rows = o.F + o.Ht + o.Wd if o.F else len(cos)
+            shape = (rows, o.rot // 2)
+            cos, sin = x.flat(cos, shape, torch.float32), x.flat(sin, shape, torch.float32)
+            o.rows = rows
+        else:
+            cos = sin = None
+        span = (lambda s: (s[1] * s[3],)) if o.norm == NORM_TOKEN else (lambda s: (s[3],))
+        return x, span, (C.byref(self.shape), C.byref(o), x.view(q, sq), x.view(k, sk),
+                         x.flat(q_weight, span(sq), torch.float32), x.flat(k_weight, span(sk), torch.float32), cos, sin,
+                         x.flat(pos, (sq[0], sq[2]), torch.int32))
+
+    def forward(self, q, k, q_out, k_out, q_weight=None, k_weight=None, cos=None, sin=None, pos=None, stream=None):
+        """q_out, k_out = the normed and turned q, k (k and k_out None with Hk = 0)."""
+        x, _, args = self._common("vc_norm_rope", q, k, q_weight, k_weight, cos, sin, pos)
+        sq, sk = self._sizes
+        self._call("vc_norm_rope", stream, *args, x.view(q_out, sq), x.view(k_out, sk))
+
+    def backward(self, q, k, dq_out, dk_out, dq, dk, q_weight=None, k_weight=None, dq_weight=None, dk_weight=None,
+                 cos=None, sin=None, pos=None, stream=None):
+        """dq, dk (and dq_weight, dk_weight where given) = the gradients of q, k and of the weights."""
+        import torch
+        fn = "vc_norm_rope_backward"
+        x, span, args = self._common(fn, q, k, q_weight, k_weight, cos, sin, pos)
+        sq, sk = self._sizes
+        self._call(fn, stream, *args, x.view(dq_out, sq), x.view(dk_out, sk), x.view(dq, sq), x.view(dk, sk),
+                   x.flat(dq_weight, span(sq), torch.float32), x.flat(dk_weight, span(sk), torch.float32),
+                   None if self.ws is None else self.ws.data_ptr(), 0 if self.ws is None else self.ws.numel())

@@ -11,7 +11,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(ROOT, "_build")
 LIB = os.path.join(HERE, "libvcattn.so")
-SOURCES = ["api.hip", "prep.hip", "forward.hip", "group.hip"]
+SOURCES = ["api.hip", "prep.hip", "forward.hip", "group.hip", "block_api.hip", "norm_rope.hip"]
 HEADERS = ["vc_common.hpp", "vc_internal.hpp"]
 PROBE = os.path.join(HERE, "mfma_probe")
 

@@ -9,8 +9,18 @@
 #include "vc_internal.hpp"
 
 namespace {
-
 thread_local int g_last_hip = 0;
+}
+
+vc_status vc::hip_status(hipError_t e) {
+  if (e == hipSuccess) return VC_OK;
+  g_last_hip = (int)e;
+  return VC_ERR_HIP;
+}
+
+namespace {
+
+using vc::hip_status;
 
 constexpr int kD = 128;
 constexpr int kKMax = 64;
@@ -110,12 +120,6 @@ int assign_tokens(int BH, int N) {
     }
   }
   return 256 * best;
-}
-
-vc_status hip_status(hipError_t e) {
-  if (e == hipSuccess) return VC_OK;
-  g_last_hip = (int)e;
-  return VC_ERR_HIP;
 }
 
 // Preprocessing workspace of vc_attn_prep_noalloc: one copy per GPU, held until the process ends.

@@ -1,0 +1,237 @@
+// C ABI of the operators around the attention (declared in include/vc_attn.h): argument validation on the
+// host, workspace carve-up and launches of the norms with the rotation.
+#include <cmath>
+#include <cstdint>
+
+#include "vc_attn.h"
+#include "vc_internal.hpp"
+
+namespace {
+
+inline bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+// A view of [B, H, n] rows of d channels; outputs must not overlap themselves
+vc_status check_view(const vc_view* v, int B, int H, int n, int d, bool output) {
+  if (!v || !v->data) return VC_ERR_NULL;
+  if (!aligned(v->data, 16)) return VC_ERR_ALIGN;
+  int64_t stride[3] = {v->sb, v->sh, v->sn}, extent[3] = {B, H, n};
+  for (int i = 0; i < 3; ++i) {
+    if (extent[i] == 1) continue;
+    if (stride[i] < 0 || stride[i] > (1LL << 40) / (extent[i] - 1)) return VC_ERR_SHAPE;
+    if (stride[i] % 8 != 0) return VC_ERR_ALIGN;
+  }
+  if (!output) return VC_OK;
+  for (int i = 0; i < 3; ++i)
+    for (int j = i + 1; j < 3; ++j)
+      if (stride[j] < stride[i]) {
+        const int64_t s = stride[i], e = extent[i];
+        stride[i] = stride[j], extent[i] = extent[j];
+        stride[j] = s, extent[j] = e;
+      }
+  int64_t span = d;
+  for (int i = 0; i < 3; ++i) {
+    if (extent[i] == 1) continue;
+    if (stride[i] < span) return VC_ERR_SHAPE;
+    span += stride[i] * (extent[i] - 1);
+  }
+  return VC_OK;
+}
+
+// strides of axes of extent 1 are not used
+void strides(const vc_view* v, int B, int H, int n, int64_t& sb, int64_t& sh, int64_t& sn) {
+  sb = B == 1 ? 0 : v->sb;
+  sh = H == 1 ? 0 : v->sh;
+  sn = n == 1 ? 0 : v->sn;
+}
+
+vc_status check_norm_rope(const vc_norm_rope_shape* s, const vc_norm_rope_opts* o) {
+  if (!s || !o) return VC_ERR_NULL;
+  if (s->B < 1 || s->N < 1 || s->Hq < 1 || s->Hk < 0 || (s->d != 64 && s->d != 128)) return VC_ERR_SHAPE;
+  if ((int64_t)s->B * s->N >= (1LL << 31) || ((int64_t)s->Hq + s->Hk) * s->d > (1 << 20)) return VC_ERR_SHAPE;
+  if (o->dtype != VC_BF16 && o->dtype != VC_FP16) return VC_ERR_UNSUPPORTED;
+  if (o->norm != VC_NORM_NONE && o->norm != VC_NORM_HEAD && o->norm != VC_NORM_TOKEN) return VC_ERR_UNSUPPORTED;
+  if (o->layout != VC_ROPE_NONE && o->layout != VC_ROPE_INTERLEAVED && o->layout != VC_ROPE_HALF)
+    return VC_ERR_UNSUPPORTED;
+  if (o->norm == VC_NORM_NONE && o->layout == VC_ROPE_NONE) return VC_ERR_UNSUPPORTED;
+  if (o->norm != VC_NORM_NONE && !(o->eps > 0.f && std::isfinite(o->eps))) return VC_ERR_UNSUPPORTED;
+  if (o->norm == VC_NORM_TOKEN && (s->Hq * s->d > 8192 || s->Hk * s->d > 8192)) return VC_ERR_SHAPE;
+  if (o->layout == VC_ROPE_NONE) return o->rot == 0 ? VC_OK : VC_ERR_UNSUPPORTED;
+  if (o->rot < 16 || o->rot > s->d || o->rot % 16 != 0) return VC_ERR_UNSUPPORTED;
+  if (o->F == 0 && o->Ht == 0 && o->Wd == 0) return o->rows >= 1 ? VC_OK : VC_ERR_UNSUPPORTED;
+  if (o->F < 1 || o->Ht < 1 || o->Wd < 1) return VC_ERR_UNSUPPORTED;
+  const int64_t fh = (int64_t)o->F * o->Ht;
+  if (fh > s->N || fh * o->Wd != s->N) return VC_ERR_SHAPE;
+  if (s->d != 128 || o->rot != 128) return VC_ERR_UNSUPPORTED;
+  return VC_OK;
+}
+
+// columns of a tensor's weights
+int norm_weights(const vc_norm_rope_opts* o, int H, int d) { return o->norm == VC_NORM_TOKEN ? H * d : d; }
+
+vc_status norm_rope_args(const vc_norm_rope_shape* s, const vc_norm_rope_opts* o, const float* cos_t,
+                         const float* sin_t, const int32_t* pos, vc::NormRopeArgs& a) {
+  const bool turned = o->layout != VC_ROPE_NONE, grid = turned && o->F > 0;
+  if (turned && (!cos_t || !sin_t)) return VC_ERR_NULL;
+  if (turned && (!aligned(cos_t, 16) || !aligned(sin_t, 16))) return VC_ERR_ALIGN;
+  if (pos && !aligned(pos, 4)) return VC_ERR_ALIGN;
+  if (grid && pos) return VC_ERR_UNSUPPORTED;
+  if (turned && !grid && !pos && o->rows < s->N) return VC_ERR_SHAPE;
+  a.ntensors = s->Hk > 0 ? 2 : 1;
+  a.tokens = (int64_t)s->B * s->N;
+  a.N = s->N;
+  a.d = s->d;
+  a.dtype = o->dtype;
+  a.norm = o->norm;
+  a.layout = o->layout;
+  a.rot = o->rot;
+  a.eps = o->eps;
+  a.sign = 1.f;
+  a.cos_t = cos_t;
+  a.sin_t = sin_t;
+  a.pos = turned ? pos : nullptr;
+  a.rows = o->rows;
+  a.grid = grid;
+  a.F = o->F;
+  a.Ht = o->Ht;
+  a.Wd = o->Wd;
+  return VC_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+vc_status vc_norm_rope(const vc_norm_rope_shape* shape, const vc_norm_rope_opts* opts, const vc_view* q,
+                       const vc_view* k, const float* q_weight, const float* k_weight, const float* rope_cos,
+                       const float* rope_sin, const int32_t* pos, const vc_view* q_out, const vc_view* k_out,
+                       void* stream) {
+  vc_status st = check_norm_rope(shape, opts);
+  if (st != VC_OK) return st;
+  vc::NormRopeArgs a{};
+  if ((st = norm_rope_args(shape, opts, rope_cos, rope_sin, pos, a)) != VC_OK) return st;
+  const int B = shape->B, N = shape->N, d = shape->d, heads[2] = {shape->Hq, shape->Hk};
+  const vc_view *in[2] = {q, k}, *out[2] = {q_out, k_out};
+  const float* weight[2] = {q_weight, k_weight};
+  for (int i = 0; i < a.ntensors; ++i) {
+    vc::NormRopeTensor& t = a.t[i];
+    if ((st = check_view(in[i], B, heads[i], N, d, false)) != VC_OK) return st;
+    if ((st = check_view(out[i], B, heads[i], N, d, true)) != VC_OK) return st;
+    if (weight[i] && !aligned(weight[i], 16)) return VC_ERR_ALIGN;
+    t.in = static_cast<const uint16_t*>(in[i]->data);
+    t.out = static_cast<uint16_t*>(out[i]->data);
+    strides(in[i], B, heads[i], N, t.in_sb, t.in_sh, t.in_sn);
+    strides(out[i], B, heads[i], N, t.out_sb, t.out_sh, t.out_sn);
+    t.weight = opts->norm == VC_NORM_NONE ? nullptr : weight[i];
+    t.H = heads[i];
+    t.weights = norm_weights(opts, t.H, d);
+    t.inv_span = 1.f / (float)t.weights;
+  }
+  return vc::hip_status(vc::launch_norm_rope(a, static_cast<hipStream_t>(stream)));
+}
+
+size_t vc_norm_rope_workspace_size(const vc_norm_rope_shape* shape, const vc_norm_rope_opts* opts) {
+  if (check_norm_rope(shape, opts) != VC_OK) return (size_t)-1;
+  if (opts->norm == VC_NORM_NONE) return 0;
+  const size_t C = norm_weights(opts, shape->Hq, shape->d) + (shape->Hk ? norm_weights(opts, shape->Hk, shape->d) : 0);
+  return C * 4 * vc::norm_rope_parts((int64_t)shape->B * shape->N);
+}
+
+vc_status vc_norm_rope_backward(const vc_norm_rope_shape* shape, const vc_norm_rope_opts* opts, const vc_view* q,
+                                const vc_view* k, const float* q_weight, const float* k_weight, const float* rope_cos,
+                                const float* rope_sin, const int32_t* pos, const vc_view* dq_out,
+                                const vc_view* dk_out, const vc_view* dq, const vc_view* dk, float* dq_weight,
+                                float* dk_weight, void* ws, size_t ws_bytes, void* stream) {
+  vc_status st = check_norm_rope(shape, opts);
+  if (st != VC_OK) return st;
+  vc::NormRopeArgs a{};
+  if ((st = norm_rope_args(shape, opts, rope_cos, rope_sin, pos, a)) != VC_OK) return st;
+  const bool norm = opts->norm != VC_NORM_NONE;
+  if (!norm && (dq_weight || dk_weight)) return VC_ERR_UNSUPPORTED;
+  const int B = shape->B, N = shape->N, d = shape->d, heads[2] = {shape->Hq, shape->Hk};
+  const vc_view *in[2] = {q, k}, *grad[2] = {dq_out, dk_out}, *out[2] = {dq, dk};
+  const float* weight[2] = {q_weight, k_weight};
+  float* dw[2] = {dq_weight, dk_weight};
+  if (dq_weight || (dk_weight && a.ntensors == 2)) {
+    if (!ws || ws_bytes < vc_norm_rope_workspace_size(shape, opts)) return VC_ERR_WORKSPACE;
+    if (!aligned(ws, 16)) return VC_ERR_ALIGN;
+  }
+  float* part = static_cast<float*>(ws);
+  for (int i = 0; i < a.ntensors; ++i) {
+    vc::NormRopeTensor& t = a.t[i];
+    if (norm && (st = check_view(in[i], B, heads[i], N, d, false)) != VC_OK) return st;
+    if ((st = check_view(grad[i], B, heads[i], N, d, false)) != VC_OK) return st;
+    if ((st = check_view(out[i], B, heads[i], N, d, true)) != VC_OK) return st;
+    if ((weight[i] && !aligned(weight[i], 16)) || (dw[i] && !aligned(dw[i], 16))) return VC_ERR_ALIGN;
+    if (norm) {
+      t.in = static_cast<const uint16_t*>(in[i]->data);
+      strides(in[i], B, heads[i], N, t.in_sb, t.in_sh, t.in_sn);
+    }
+    t.grad = static_cast<const uint16_t*>(grad[i]->data);
+    t.out = static_cast<uint16_t*>(out[i]->data);
+    strides(grad[i], B, heads[i], N, t.grad_sb, t.grad_sh, t.grad_sn);
+    strides(out[i], B, heads[i], N, t.out_sb, t.out_sh, t.out_sn);
+    t.weight = norm ? weight[i] : nullptr;
+    t.H = heads[i];
+    t.weights = norm_weights(opts, t.H, d);
+    t.inv_span = 1.f / (float)t.weights;
+    t.dw = dw[i];
+    if (dw[i]) {
+      t.dw_part = part;
+      part += (size_t)t.weights * vc::norm_rope_parts(a.tokens);
+    }
+  }
+  if (!norm) {
+    // the rotation's gradient: the rotation with the sines negated
+    for (int i = 0; i < a.ntensors; ++i) {
+      vc::NormRopeTensor& t = a.t[i];
+      t.in = t.grad;
+      t.in_sb = t.grad_sb, t.in_sh = t.grad_sh, t.in_sn = t.grad_sn;
+    }
+    a.sign = -1.f;
+    return vc::hip_status(vc::launch_norm_rope(a, static_cast<hipStream_t>(stream)));
+  }
+  return vc::hip_status(vc::launch_norm_rope_backward(a, static_cast<hipStream_t>(stream)));
+}
+
+vc_status vc_rope_line_tables(int32_t rows, int32_t rot, double theta, const vc_rope_scaling* scaling, float* cos_t,
+                              float* sin_t) {
+  if (!cos_t || !sin_t) return VC_ERR_NULL;
+  if (rows < 1 || rot < 16 || rot > 128 || rot % 16 != 0 || (int64_t)rows * (rot / 2) >= (1LL << 31))
+    return VC_ERR_SHAPE;
+  if (!(theta > 0.0) || !std::isfinite(theta)) return VC_ERR_SHAPE;
+  const int half = rot / 2;
+  double magnitude = 1.0, freq[64];
+  for (int i = 0; i < half; ++i) freq[i] = std::pow(theta, -2.0 * i / rot);
+  if (scaling) {
+    const vc_rope_scaling& c = *scaling;
+    if (c.kind < VC_SCALE_NONE || c.kind > VC_SCALE_PARTS) return VC_ERR_UNSUPPORTED;
+    if (c.kind != VC_SCALE_NONE && !(c.factor >= 1.0 && std::isfinite(c.factor))) return VC_ERR_UNSUPPORTED;
+    if (!(c.magnitude >= 0.0) || !std::isfinite(c.magnitude)) return VC_ERR_UNSUPPORTED;
+    if (c.magnitude > 0.0) magnitude = c.magnitude;
+    if (c.kind == VC_SCALE_LINEAR)
+      for (int i = 0; i < half; ++i) freq[i] /= c.factor;
+    if (c.kind == VC_SCALE_BASE) {
+      const double base = theta * std::pow(c.factor, (double)rot / (rot - 2));
+      for (int i = 0; i < half; ++i) freq[i] = std::pow(base, -2.0 * i / rot);
+    }
+    if (c.kind == VC_SCALE_PARTS) {
+      if (!(c.trained >= 1.0 && std::isfinite(c.trained) && c.slow >= 0.0 && c.fast > c.slow && std::isfinite(c.fast)))
+        return VC_ERR_UNSUPPORTED;
+      for (int i = 0; i < half; ++i) {
+        const double turns = c.trained * freq[i] / 6.283185307179586476925;
+        double keep = (turns - c.slow) / (c.fast - c.slow);
+        keep = keep < 0.0 ? 0.0 : (keep > 1.0 ? 1.0 : keep);
+        freq[i] = freq[i] * keep + freq[i] / c.factor * (1.0 - keep);
+      }
+    }
+  }
+  for (int p = 0; p < rows; ++p)
+    for (int i = 0; i < half; ++i) {
+      const double ang = (double)p * freq[i];
+      cos_t[(size_t)p * half + i] = (float)(std::cos(ang) * magnitude);
+      sin_t[(size_t)p * half + i] = (float)(std::sin(ang) * magnitude);
+    }
+  return VC_OK;
+}
+
+}  // extern "C"

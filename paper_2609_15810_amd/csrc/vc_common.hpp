@@ -26,6 +26,15 @@ __device__ __forceinline__ uint16_t f32_to_bf16(float f) {
   return __builtin_bit_cast(uint16_t, b);
 }
 
+// two fp32 values -> two bf16 (DT = VC_BF16 = 0) or fp16 (1) values, round to nearest even
+template <int DT>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+  typedef _Float16 f2 __attribute__((ext_vector_type(2)));
+  if constexpr (DT == 0) return __builtin_bit_cast(uint32_t, __builtin_convertvector((v2f){lo, hi}, b2));
+  else return __builtin_bit_cast(uint32_t, __builtin_convertvector((v2f){lo, hi}, f2));
+}
+
 // Byte offset inside one 128x128 int8 block of Q or K codes, tiled for the INT8 matrix
 // instruction: [rb 4][dc 4][dh 2][r 32][e 16].
 __host__ __device__ __forceinline__ int qk_tile_offset(int row, int ch) {

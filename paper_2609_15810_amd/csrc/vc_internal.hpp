@@ -74,12 +74,45 @@ struct GroupArgs {
   int atok;           // tokens per assignment workgroup (a multiple of 256)
 };
 
+// One of the tensors (queries, keys) of the norm and rotation: rows [b, h, n] of d channels at element
+// strides, and for the backward pass the gradient of its output (grad) with out the gradient of its input
+struct NormRopeTensor {
+  const uint16_t *in, *grad;
+  uint16_t* out;
+  int64_t in_sb, in_sh, in_sn, grad_sb, grad_sh, grad_sn, out_sb, out_sh, out_sn;
+  const float* weight;   // of the norm, or null (ones)
+  float* dw;
+  float* dw_part;        // [workgroups][weights] partial sums, or null (no weight gradient)
+  float inv_span;        // 1 / channels under one norm
+  int H, weights;
+  int P, parts, iters;   // head slots of a wave; waves that share a token's heads; iterations of a wave over them
+};
+
+struct NormRopeArgs {
+  NormRopeTensor t[2];
+  int ntensors;
+  int64_t tokens;        // B * N
+  int N, d, dtype, norm, layout, rot;
+  float eps, sign;       // sign of the sines
+  const float *cos_t, *sin_t;
+  const int32_t* pos;    // [B][N] table rows, or null
+  int rows;              // of the tables on a line
+  int grid, F, Ht, Wd;   // grid: positions on the latent grid, tables of frames, rows and columns
+};
+
 hipError_t launch_prep(const PrepArgs& a, int BH, hipStream_t s);
 ForwardPlan forward_plan(int N, int BH, int qk_fmt, int p_mode);
 hipError_t launch_forward(FwdArgs a, int BH, hipStream_t s);
 hipError_t launch_group(const GroupArgs& a, int BH, hipStream_t s);
 hipError_t launch_fp8_score_product(const uint8_t* a, const uint8_t* b, const float* c_in, float* out, int n,
                                     hipStream_t s);
+
+hipError_t launch_norm_rope(NormRopeArgs a, hipStream_t s);
+hipError_t launch_norm_rope_backward(NormRopeArgs a, hipStream_t s);
+int norm_rope_parts(int64_t tokens);   // workgroups of the backward kernel
+
+// VC_OK, or VC_ERR_HIP with the error kept for vc_last_hip_error
+vc_status hip_status(hipError_t e);
 
 }  // namespace vc
 
