@@ -384,6 +384,65 @@ typedef struct {
 vc_status vc_rope_line_tables(int32_t rows, int32_t rot, double theta, const vc_rope_scaling *scaling, float *cos_t,
                               float *sin_t);
 
+/* Shape of the attention to another sequence: B items, Hq query heads of M queries, Hk key heads of N keys, d = 64 or
+ * 128 channels; query head h attends to key head h / (Hq / Hk). All sizes >= 1, Hq a multiple of Hk,
+ * B * Hq * M < 2^31, B * Hk * N < 2^31 and (Hq / Hk) * M, N <= 2^30 (VC_ERR_SHAPE otherwise). */
+typedef struct {
+    int32_t B, Hq, Hk, M, N, d;
+} vc_cross_shape;
+
+/* Options of the attention to another sequence.
+ *   dtype    : VC_BF16 or VC_FP16, of all tensors. The products take 16-bit operands: the probabilities (and in the
+ *              backward pass their gradients) are rounded to dtype before they enter a product. Sums and the softmax's
+ *              statistics are fp32, outputs are rounded once. With VC_FP16, gradients of scores (dS, of the size of
+ *              dO times V) have fp16's range: a loss scaled as for any fp16 training keeps them there.
+ *   sm_scale : score scale, >= 0 with sm_scale * log2(e) finite in fp32; 0 selects 1/sqrt(d).
+ *   masked   : 1 = the calls give a k_mask (the workspace then holds the list of the keys that count), else 0.
+ * VC_ERR_UNSUPPORTED for a value outside these. */
+typedef struct {
+    int32_t dtype;
+    float sm_scale;
+    int32_t masked;
+} vc_cross_opts;
+
+/* Bytes of device workspace that vc_cross_attn_forward (backward = 0) or vc_cross_attn_backward (1) needs; may be 0.
+ * Returns (size_t)-1 if the shape or options are invalid. */
+size_t vc_cross_attn_workspace_size(const vc_cross_shape *shape, const vc_cross_opts *opts, int32_t backward);
+
+/* Attention to the states of another sequence (an encoder's): O = softmax(sm_scale Q K^T) V, without causality.
+ *   Q        : [B, Hq, M, d].  K, V : [B, Hk, N, d].  O : [B, Hq, M, d], written; it must not overlap an input.
+ *   k_len    : int32 [B], 4-byte aligned, device: only the first k_len[b] keys of item b count (clamped to [0, N]);
+ *              NULL: all.
+ *   k_mask   : uint8 [B, N] at row stride k_mask_stride (>= N, or 0: one row for all items): keys of value 0 do not
+ *              count. NULL exactly if opts->masked = 0 (VC_ERR_NULL / VC_ERR_UNSUPPORTED otherwise). Together with k_len
+ *              a key has to pass both.
+ *              K and V of keys that do not count are not read: they may hold anything, NaN too. A query all of
+ *              whose keys do not count gets O = 0 and lse = -inf.
+ *   lse      : fp32 [B, Hq, M] contiguous, 4-byte aligned: natural logarithm of the sum of exp(score), written for
+ *              vc_cross_attn_backward; NULL: not written.
+ *   ws       : device workspace of ws_bytes >= vc_cross_attn_workspace_size(shape, opts, 0), 16-byte aligned (may be
+ *              NULL if that is 0). Its content need not be kept from call to call; calls that overlap in time need one
+ *              each.
+ * The same operands, shape and options give the same bits in every call. */
+vc_status vc_cross_attn_forward(const vc_cross_shape *shape, const vc_cross_opts *opts, const vc_view *Q,
+                                const vc_view *K, const vc_view *V, const int32_t *k_len, const uint8_t *k_mask,
+                                int64_t k_mask_stride, const vc_view *O, float *lse, void *ws, size_t ws_bytes,
+                                void *stream);
+
+/* Gradients of vc_cross_attn_forward.
+ *   Q, K, V, k_len, k_mask, O, lse : as given to and written by vc_cross_attn_forward.
+ *   dO         : gradient of O, [B, Hq, M, d].
+ *   dQ, dK, dV : gradients, written (not added to), shapes of Q, K, V; they must not overlap an input or each other.
+ *                dK and dV are summed over the query heads of their key head; where K or V is shared along an axis by a
+ *                stride of 0, they are the gradients of each copy. Rows of keys that do not count are written as 0,
+ *                and so is dQ where no key counts.
+ *   ws         : ws_bytes >= vc_cross_attn_workspace_size(shape, opts, 1). */
+vc_status vc_cross_attn_backward(const vc_cross_shape *shape, const vc_cross_opts *opts, const vc_view *Q,
+                                 const vc_view *K, const vc_view *V, const int32_t *k_len, const uint8_t *k_mask,
+                                 int64_t k_mask_stride, const vc_view *O, const float *lse, const vc_view *dO,
+                                 const vc_view *dQ, const vc_view *dK, const vc_view *dV, void *ws, size_t ws_bytes,
+                                 void *stream);
+
 /* Static description of a status code. */
 const char *vc_status_str(vc_status s);
 

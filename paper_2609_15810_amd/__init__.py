@@ -63,6 +63,14 @@ class View(C.Structure):
     _fields_ = [("data", C.c_void_p), ("sb", C.c_int64), ("sh", C.c_int64), ("sn", C.c_int64)]
 
 
+class CrossShape(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("B", "Hq", "Hk", "M", "N", "d")]
+
+
+class CrossOpts(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("sm_scale", C.c_float), ("masked", C.c_int32)]
+
+
 class NormRopeShape(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("B", "Hq", "Hk", "N", "d")]
 
@@ -113,6 +121,14 @@ def lib():
                                             C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
         L.vc_fp8_score_product.restype = C.c_int
         L.vc_fp8_score_product.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p]
+        L.vc_cross_attn_workspace_size.restype = C.c_size_t
+        L.vc_cross_attn_workspace_size.argtypes = [C.POINTER(CrossShape), C.POINTER(CrossOpts), C.c_int32]
+        inputs = [C.POINTER(CrossShape), C.POINTER(CrossOpts)] + [C.POINTER(View)] * 3 + \
+            [C.c_void_p, C.c_void_p, C.c_int64, C.POINTER(View), C.c_void_p]
+        L.vc_cross_attn_forward.restype = C.c_int
+        L.vc_cross_attn_forward.argtypes = inputs + [C.c_void_p, C.c_size_t, C.c_void_p]
+        L.vc_cross_attn_backward.restype = C.c_int
+        L.vc_cross_attn_backward.argtypes = inputs + [C.POINTER(View)] * 4 + [C.c_void_p, C.c_size_t, C.c_void_p]
         L.vc_norm_rope.restype = C.c_int
         L.vc_norm_rope.argtypes = [C.POINTER(NormRopeShape), C.POINTER(NormRopeOpts)] + [C.POINTER(View)] * 2 + \
             [C.c_void_p] * 5 + [C.POINTER(View)] * 2 + [C.c_void_p]
@@ -449,3 +465,54 @@ class NormRope(_Operator):
         self._call(fn, stream, *args, x.view(dq_out, sq), x.view(dk_out, sk), x.view(dq, sq), x.view(dk, sk),
                    x.flat(dq_weight, span(sq), torch.float32), x.flat(dk_weight, span(sk), torch.float32),
                    None if self.ws is None else self.ws.data_ptr(), 0 if self.ws is None else self.ws.numel())
+
+
+class CrossAttention(_Operator):
+    """Attention to the states of another sequence for one shape: vc_cross_attn_forward and its gradients.
+
+    Q, O (and dO, dQ) are [B, Hq, M, d], K, V (dK, dV) [B, Hk, N, d] of `dtype` in any strides whose channels
+    are contiguous. k_len: int32 [B]; k_mask (with masked=True): uint8 or bool [B, N], nonzero where a key counts.
+    training: also hold the workspace of backward(). Two calls that overlap in time (on two streams, or two captured
+    graphs) need an object each: both calls use the object's workspace.
+    """
+
+    def __init__(self, B, Hq, Hk, M, N, d=D, dtype=None, sm_scale=0.0, masked=False, training=False, device="cuda"):
+        import torch
+        super().__init__(torch.bfloat16 if dtype is None else dtype, device)
+        self.shape = CrossShape(B, Hq, Hk, M, N, d)
+        self.opts = CrossOpts(self.c_dtype, sm_scale, int(bool(masked)))
+        size = 0
+        for backward in range(2 if training else 1):
+            need = lib().vc_cross_attn_workspace_size(C.byref(self.shape), C.byref(self.opts), backward)
+            if need == C.c_size_t(-1).value:
+                raise VcError("vc_cross_attn_workspace_size", 2, lib())
+            size = max(size, need)
+        self.training = bool(training)
+        self.ws = torch.empty(max(size, 16), dtype=torch.uint8, device=self.device)
+        self._q, self._k = (B, Hq, M, d), (B, Hk, N, d)
+
+    def _inputs(self, fn, Q, K, V, k_len, k_mask, O, lse):
+        import torch
+        x, (B, Hq, M, _), N = _Operands(fn, self.dtype, self.device), self._q, self._k[2]
+        stride = 0
+        if k_mask is not None:
+            if tuple(k_mask.shape) != (B, N) or k_mask.dtype not in (torch.uint8, torch.bool) or \
+                    k_mask.device != self.device:
+                x.refuse(2)
+            if k_mask.stride(1) != 1 and N > 1:
+                x.refuse(5)
+            stride = k_mask.stride(0)
+        return x, (C.byref(self.shape), C.byref(self.opts), x.view(Q, self._q), x.view(K, self._k), x.view(V, self._k),
+                   x.flat(k_len, (B,), torch.int32), None if k_mask is None else k_mask.data_ptr(), stride,
+                   x.view(O, self._q), x.flat(lse, (B, Hq, M), torch.float32))
+
+    def forward(self, Q, K, V, O, lse=None, k_len=None, k_mask=None, stream=None):
+        """O = softmax(sm_scale Q K^T) V; lse [B, Hq, M] fp32 is written where given (for backward)."""
+        _, args = self._inputs("vc_cross_attn_forward", Q, K, V, k_len, k_mask, O, lse)
+        self._call("vc_cross_attn_forward", stream, *args, self.ws.data_ptr(), self.ws.numel())
+
+    def backward(self, Q, K, V, O, lse, dO, dQ, dK, dV, k_len=None, k_mask=None, stream=None):
+        """dQ, dK, dV from dO, with O and lse as forward() wrote them."""
+        x, args = self._inputs("vc_cross_attn_backward", Q, K, V, k_len, k_mask, O, lse)
+        self._call("vc_cross_attn_backward", stream, *args, x.view(dO, self._q), x.view(dQ, self._q),
+                   x.view(dK, self._k), x.view(dV, self._k), self.ws.data_ptr(), self.ws.numel())

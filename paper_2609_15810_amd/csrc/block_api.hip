@@ -1,5 +1,5 @@
 // C ABI of the operators around the attention (declared in include/vc_attn.h): argument validation on the
-// host, workspace carve-up and launches of the norms with the rotation.
+// host, workspace carve-up and launches of the norms with the rotation and of the attention to another sequence.
 #include <cmath>
 #include <cstdint>
 
@@ -97,9 +97,141 @@ vc_status norm_rope_args(const vc_norm_rope_shape* s, const vc_norm_rope_opts* o
   return VC_OK;
 }
 
+vc_status check_cross(const vc_cross_shape* s, const vc_cross_opts* o) {
+  if (!s || !o) return VC_ERR_NULL;
+  if (s->B < 1 || s->Hq < 1 || s->Hk < 1 || s->M < 1 || s->N < 1 || (s->d != 64 && s->d != 128)) return VC_ERR_SHAPE;
+  if (s->Hq % s->Hk != 0) return VC_ERR_SHAPE;
+  const int64_t top = 1LL << 31;
+  if ((int64_t)s->B * s->Hq >= top || (int64_t)s->B * s->Hq * s->M >= top || (int64_t)s->B * s->Hk * s->N >= top)
+    return VC_ERR_SHAPE;
+  if ((int64_t)(s->Hq / s->Hk) * s->M > (1 << 30) || s->N > (1 << 30)) return VC_ERR_SHAPE;
+  if (o->dtype != VC_BF16 && o->dtype != VC_FP16) return VC_ERR_UNSUPPORTED;
+  if (!(o->sm_scale >= 0.f) || !std::isfinite(o->sm_scale * 1.4426950408889634f)) return VC_ERR_UNSUPPORTED;
+  if (o->masked != 0 && o->masked != 1) return VC_ERR_UNSUPPORTED;
+  return VC_OK;
+}
+
+inline size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
+
+// The shape, the plan and the workspace of a call: fills a, returns the bytes that the workspace at `ws` takes
+size_t cross_args(const vc_cross_shape* s, const vc_cross_opts* o, bool backward, void* ws, vc::CrossArgs& a) {
+  a.B = s->B;
+  a.Hq = s->Hq;
+  a.Hk = s->Hk;
+  a.G = s->Hq / s->Hk;
+  a.M = s->M;
+  a.N = s->N;
+  a.R = a.G * a.M;
+  a.d = s->d;
+  a.dtype = o->dtype;
+  const double scale = o->sm_scale > 0.f ? (double)o->sm_scale : 1.0 / std::sqrt((double)s->d);
+  a.scale = (float)scale;
+  a.c = (float)(scale * 1.4426950408889634074);
+  if (backward) vc::cross_plan_backward(a);
+  else vc::cross_plan(a);
+  size_t end = 0;
+  auto part = [&](size_t bytes) {
+    const size_t at = end;
+    end += align256(bytes);
+    return static_cast<char*>(ws) + at;
+  };
+  const size_t rows = (size_t)a.B * a.Hk * a.R, keys = (size_t)a.B * a.Hk * a.N;
+  if (o->masked) {
+    a.idx = reinterpret_cast<int32_t*>(part((size_t)a.B * a.N * 4));
+    a.count = reinterpret_cast<int32_t*>(part((size_t)a.B * 4));
+  }
+  if (a.splits > 1) {
+    a.part_o = reinterpret_cast<float*>(part(a.splits * rows * a.d * 4));
+    if (!backward) a.part_ml = reinterpret_cast<float*>(part(a.splits * rows * 8));
+  }
+  if (backward) {
+    a.stats = reinterpret_cast<float*>(part((size_t)a.B * a.Hk * vc::cross_stat_rows(a.R) * 8));
+    if (a.row_splits > 1) a.part_kv = reinterpret_cast<float*>(part(a.row_splits * 2 * keys * a.d * 4));
+  }
+  return end;
+}
+
+vc_status cross_view(const vc_view* v, int B, int H, int n, int d, bool output, vc::Strided& t) {
+  const vc_status st = check_view(v, B, H, n, d, output);
+  if (st != VC_OK) return st;
+  t.p = static_cast<uint16_t*>(v->data);
+  strides(v, B, H, n, t.sb, t.sh, t.sn);
+  return VC_OK;
+}
+
+// The arguments that both directions share
+vc_status cross_inputs(const vc_cross_shape* s, const vc_cross_opts* o, const vc_view* Q, const vc_view* K,
+                       const vc_view* V, const int32_t* k_len, const uint8_t* k_mask, int64_t stride, void* ws,
+                       size_t ws_bytes, bool backward, vc::CrossArgs& a) {
+  vc_status st = check_cross(s, o);
+  if (st != VC_OK) return st;
+  if ((st = cross_view(Q, s->B, s->Hq, s->M, s->d, false, a.Q)) != VC_OK) return st;
+  if ((st = cross_view(K, s->B, s->Hk, s->N, s->d, false, a.K)) != VC_OK) return st;
+  if ((st = cross_view(V, s->B, s->Hk, s->N, s->d, false, a.V)) != VC_OK) return st;
+  if (k_len && !aligned(k_len, 4)) return VC_ERR_ALIGN;
+  if (o->masked && !k_mask) return VC_ERR_NULL;
+  if (!o->masked && k_mask) return VC_ERR_UNSUPPORTED;
+  if (k_mask && s->B > 1 && stride != 0 && stride < s->N) return VC_ERR_SHAPE;
+  a.k_len = k_len;
+  const size_t need = cross_args(s, o, backward, ws, a);
+  if (need > 0 && (!ws || ws_bytes < need)) return VC_ERR_WORKSPACE;
+  if (need > 0 && !aligned(ws, 16)) return VC_ERR_ALIGN;
+  return VC_OK;
+}
+
+// the list of the keys that count, where there is a mask
+vc_status cross_keys(const vc::CrossArgs& a, const uint8_t* k_mask, int64_t stride, hipStream_t s) {
+  if (!k_mask) return VC_OK;
+  return vc::hip_status(vc::launch_cross_keys(k_mask, stride, a.k_len, a.B, a.N, const_cast<int32_t*>(a.idx),
+                                              const_cast<int32_t*>(a.count), s));
+}
+
 }  // namespace
 
 extern "C" {
+
+size_t vc_cross_attn_workspace_size(const vc_cross_shape* shape, const vc_cross_opts* opts, int32_t backward) {
+  if (check_cross(shape, opts) != VC_OK) return (size_t)-1;
+  vc::CrossArgs a{};
+  return cross_args(shape, opts, backward != 0, nullptr, a);
+}
+
+vc_status vc_cross_attn_forward(const vc_cross_shape* shape, const vc_cross_opts* opts, const vc_view* Q,
+                                const vc_view* K, const vc_view* V, const int32_t* k_len, const uint8_t* k_mask,
+                                int64_t k_mask_stride, const vc_view* O, float* lse, void* ws, size_t ws_bytes,
+                                void* stream) {
+  vc::CrossArgs a{};
+  vc_status st = cross_inputs(shape, opts, Q, K, V, k_len, k_mask, k_mask_stride, ws, ws_bytes, false, a);
+  if (st != VC_OK) return st;
+  if ((st = cross_view(O, shape->B, shape->Hq, shape->M, shape->d, true, a.O)) != VC_OK) return st;
+  if (lse && !aligned(lse, 4)) return VC_ERR_ALIGN;
+  a.lse = lse;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  if ((st = cross_keys(a, k_mask, k_mask_stride, s)) != VC_OK) return st;
+  return vc::hip_status(vc::launch_cross_forward(a, s));
+}
+
+vc_status vc_cross_attn_backward(const vc_cross_shape* shape, const vc_cross_opts* opts, const vc_view* Q,
+                                 const vc_view* K, const vc_view* V, const int32_t* k_len, const uint8_t* k_mask,
+                                 int64_t k_mask_stride, const vc_view* O, const float* lse, const vc_view* dO,
+                                 const vc_view* dQ, const vc_view* dK, const vc_view* dV, void* ws, size_t ws_bytes,
+                                 void* stream) {
+  vc::CrossArgs a{};
+  vc_status st = cross_inputs(shape, opts, Q, K, V, k_len, k_mask, k_mask_stride, ws, ws_bytes, true, a);
+  if (st != VC_OK) return st;
+  const int B = shape->B, Hq = shape->Hq, Hk = shape->Hk, M = shape->M, N = shape->N, d = shape->d;
+  if ((st = cross_view(O, B, Hq, M, d, false, a.O)) != VC_OK) return st;
+  if ((st = cross_view(dO, B, Hq, M, d, false, a.dO)) != VC_OK) return st;
+  if ((st = cross_view(dQ, B, Hq, M, d, true, a.dQ)) != VC_OK) return st;
+  if ((st = cross_view(dK, B, Hk, N, d, true, a.dK)) != VC_OK) return st;
+  if ((st = cross_view(dV, B, Hk, N, d, true, a.dV)) != VC_OK) return st;
+  if (!lse) return VC_ERR_NULL;
+  if (!aligned(lse, 4)) return VC_ERR_ALIGN;
+  a.lse = const_cast<float*>(lse);
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  if ((st = cross_keys(a, k_mask, k_mask_stride, s)) != VC_OK) return st;
+  return vc::hip_status(vc::launch_cross_backward(a, s));
+}
 
 vc_status vc_norm_rope(const vc_norm_rope_shape* shape, const vc_norm_rope_opts* opts, const vc_view* q,
                        const vc_view* k, const float* q_weight, const float* k_weight, const float* rope_cos,

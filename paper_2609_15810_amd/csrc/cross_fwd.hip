@@ -1,0 +1,294 @@
+// Attention of queries to the states of another sequence, 16-bit operands, forward.
+//
+//   O_i = sum_j p_ij v_j,  p_ij = exp(c' q_i k_j - lse_i),  lse_i = log sum_j exp(c' q_i k_j)
+//
+// over the keys j that count for the batch item. Keys are visited in tiles of 64 with a running maximum and sum; exponents
+// are in log2 units (c = c' log2 e). Both products are computed transposed so that a lane owns one query (column
+// lane % 32 of a 32x32 product): S^T = K Q^T with keys from LDS and the wave's 32 queries in registers, then
+// O^T += V^T P^T, for which the probabilities of a lane are already in operand order and V is read from LDS by
+// transposing reads. A workgroup's four waves share the tiles (128 rows); tiles are copied straight into LDS, one
+// tile ahead.
+//
+// The rows of a key head are those of all its query heads, one head behind the other, so that grouped heads share
+// tiles and a token's few queries share one.
+//
+// Few rows and long keys: the keys are split over workgroups (cross_plan), each leaves unnormalised fp32 outputs with its
+// maximum and sum, and cross_join adds them up in a fixed order.
+#include "cross_common.hpp"
+
+namespace vc {
+namespace cross {
+namespace {
+
+constexpr int NW = 4;           // waves of a workgroup
+constexpr int QR = 32 * NW;     // its rows
+constexpr int KT = 64;          // keys of a tile
+
+// IDX: the keys are those of a list (a key padding mask); SPLIT: leave parts
+template <int DT, int D, bool IDX, bool SPLIT>
+__global__ __launch_bounds__(64 * NW, 2) void cross_fwd(CrossArgs a) {
+  using T = Tile<D>;
+  constexpr int TB = KT * T::ROW;                                // bytes of a tile
+  constexpr int COPIES = KT / T::ROWS_PER_COPY / NW;             // of a wave, per tile
+  constexpr int KS = D / 16, DB = D / 32;
+  __shared__ __attribute__((aligned(16))) uint8_t kt[2][TB], vt[2][TB];
+
+  const uint32_t wg = xcd_order(blockIdx.x, gridDim.x), blocks = (uint32_t)(a.R + QR - 1) / QR;
+  const uint32_t rest = wg / blocks, bh = rest / (uint32_t)a.splits;
+  const int rb = wg - rest * blocks, split = rest - bh * a.splits;
+  const int b = bh / (uint32_t)a.Hk, hk = bh - b * a.Hk;
+  const int lane = threadIdx.x & 63, col = lane & 31, kh = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = keys_of(a, b);
+  const int k0 = SPLIT ? split * a.chunk : 0, k1 = SPLIT ? min(n, k0 + a.chunk) : n;
+  const int tiles = k1 > k0 ? (k1 - k0 + KT - 1) / KT : 0;
+
+  // the rows of a tile that this lane copies, and their tensors
+  const uint16_t *kbase = a.K.p + b * a.K.sb + hk * a.K.sh, *vbase = a.V.p + b * a.V.sb + hk * a.V.sh;
+  const int crow = lane / T::CH;
+  int next[COPIES];   // IDX: keys of the next tile to copy
+  auto fetch = [&](int t) __attribute__((always_inline)) {
+    if (IDX) {
+#pragma unroll
+      for (int u = 0; u < COPIES; ++u) {
+        const int j = k0 + t * KT + (u * NW + wave) * T::ROWS_PER_COPY + crow;
+        next[u] = j < k1 ? a.idx[(size_t)b * a.N + j] : -1;
+      }
+    }
+  };
+  auto copy_tile = [&](int t, int buf) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < COPIES; ++u) {
+      const int q = u * NW + wave, r = q * T::ROWS_PER_COPY + crow;
+      const int j = k0 + t * KT + r, ch = (lane % T::CH) ^ T::key(r);
+      const int64_t src = IDX ? next[u] : j;
+      const bool in = IDX ? next[u] >= 0 : j < k1;
+      copy16(in ? (const void*)(kbase + src * a.K.sn + 8 * ch) : (const void*)&zero16, kt[buf] + q * 1024);
+      copy16(in ? (const void*)(vbase + src * a.V.sn + 8 * ch) : (const void*)&zero16, vt[buf] + q * 1024);
+    }
+  };
+  if (tiles > 0) {
+    fetch(0);
+    copy_tile(0, 0);
+    fetch(1);
+  }
+
+  const int r0 = rb * QR + 32 * wave, row = r0 + col;
+  const bool active = r0 < a.R;   // waves without rows only copy
+  const QueryRow qr = query_row(a, hk, min(row, a.R - 1));
+  u4 q[KS];
+  {
+    const uint16_t* p = a.Q.p + b * a.Q.sb + qr.h * a.Q.sh + qr.i * a.Q.sn + 8 * kh;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) q[s] = *reinterpret_cast<const u4*>(p + 16 * s);
+  }
+  v16f o[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db) o[db] = v16f{};
+  float m = -INFINITY, l = 0.f;   // l: of this lane's keys
+
+  for (int t = 0; t < tiles; ++t) {
+    wait_copies();
+    barrier();
+    if (t + 1 < tiles) {
+      copy_tile(t + 1, (t + 1) & 1);
+      fetch(t + 2);
+    }
+    if (!active) continue;
+    const uint8_t *kb = kt[t & 1], *vb = vt[t & 1];
+    v16f s[2];
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      s[g] = v16f{};
+#pragma unroll
+      for (int i = 0; i < KS; ++i) s[g] = mma<DT>(T::rows(kb, 32 * g, i, lane), q[i], s[g]);
+    }
+    const int valid = k1 - k0 - t * KT;
+    if (valid < KT) {
+#pragma unroll
+      for (int g = 0; g < 2; ++g)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (32 * g + 8 * (r >> 2) + 4 * kh + (r & 3) >= valid) s[g][r] = -INFINITY;
+    }
+    float top = fmaxf(s[0][0], s[1][0]);
+#pragma unroll
+    for (int r = 1; r < 16; ++r) top = fmaxf(fmaxf(top, s[0][r]), s[1][r]);
+    top = half_max(top) * a.c;
+    if (__builtin_amdgcn_ballot_w64(top > m)) {
+      const float up = fmaxf(m, top), alpha = __builtin_amdgcn_exp2f(m - (up == -INFINITY ? 0.f : up));
+      m = up;
+      l *= alpha;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[db][r] *= alpha;
+    }
+    const float off = m == -INFINITY ? 0.f : m;   // scores of -inf alone so far
+#pragma unroll
+    for (int g = 0; g < 2; ++g)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float p[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[g][8 * h + e], a.c, -off));
+          l += p[e];
+        }
+        const u4 pp = {pack2<DT>(p[0], p[1]), pack2<DT>(p[2], p[3]), pack2<DT>(p[4], p[5]), pack2<DT>(p[6], p[7])};
+#pragma unroll
+        for (int db = 0; db < DB; ++db) o[db] = mma<DT>(T::cols(vb, 32 * g + 16 * h, db, lane), pp, o[db]);
+      }
+  }
+  l = half_sum(l);
+
+  if (SPLIT) {
+    if (row < a.R) {
+      const size_t at = ((size_t)split * a.B * a.Hk + bh) * a.R + row;
+      if (kh == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * at) = make_float2(m, l);
+      float* p = a.part_o + at * D + 4 * kh;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          *reinterpret_cast<float4*>(p + 32 * db + 8 * g) =
+              make_float4(o[db][4 * g], o[db][4 * g + 1], o[db][4 * g + 2], o[db][4 * g + 3]);
+    }
+    return;
+  }
+  // no key counts: O = 0, lse = -inf
+  const float inv = n > 0 ? 1.f / l : 0.f;
+  if (a.lse && row < a.R && kh == 0)
+    a.lse[((size_t)b * a.Hq + qr.h) * a.M + qr.i] = n > 0 ? (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : -INFINITY;
+  // rows leave through LDS, so that each is stored as a whole
+  barrier();
+  uint8_t* out = kt[0] + wave * 32 * T::ROW;
+  static_assert(NW * 32 <= 2 * KT, "a workgroup's rows fit the two key buffers");
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      *reinterpret_cast<u2*>(out + T::at(col, 4 * db + g) + 8 * kh) =
+          u2{pack2<DT>(o[db][4 * g] * inv, o[db][4 * g + 1] * inv), pack2<DT>(o[db][4 * g + 2] * inv, o[db][4 * g + 3] * inv)};
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+  for (int u = 0; u < 32 / T::ROWS_PER_COPY; ++u) {
+    const int r = u * T::ROWS_PER_COPY + crow, ch = lane % T::CH;
+    if (r0 + r < a.R) {
+      const QueryRow w = query_row(a, hk, r0 + r);
+      *reinterpret_cast<u4*>(a.O.p + b * a.O.sb + w.h * a.O.sh + w.i * a.O.sn + 8 * ch) =
+          *reinterpret_cast<const u4*>(out + T::at(r, ch));
+    }
+  }
+}
+
+// The parts of a row joined: d / 4 lanes a row
+template <int DT, int D>
+__global__ __launch_bounds__(256) void cross_join(CrossArgs a) {
+  constexpr int L = D / 4, ROWS = 256 / L;
+  const int64_t rows = (int64_t)a.B * a.Hk * a.R, at = (int64_t)blockIdx.x * ROWS + threadIdx.x / L;
+  if (at >= rows) return;
+  const int c = threadIdx.x % L * 4;
+  float m = -INFINITY;
+  for (int s = 0; s < a.splits; ++s) m = fmaxf(m, a.part_ml[2 * (s * rows + at)]);
+  const float off = m == -INFINITY ? 0.f : m;
+  float l = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int s = 0; s < a.splits; ++s) {
+    const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * (s * rows + at));
+    const float4 v = *reinterpret_cast<const float4*>(a.part_o + (s * rows + at) * D + c);
+    const float w = __builtin_amdgcn_exp2f(ml.x - off);
+    l = __builtin_fmaf(w, ml.y, l);
+    o.x = __builtin_fmaf(w, v.x, o.x), o.y = __builtin_fmaf(w, v.y, o.y);
+    o.z = __builtin_fmaf(w, v.z, o.z), o.w = __builtin_fmaf(w, v.w, o.w);
+  }
+  const uint32_t bh = at / a.R;
+  const int b = bh / (uint32_t)a.Hk, hk = bh - b * a.Hk, n = keys_of(a, b);
+  const QueryRow w = query_row(a, hk, (int)(at - (int64_t)bh * a.R));
+  const float inv = n > 0 ? 1.f / l : 0.f;
+  *reinterpret_cast<u2*>(a.O.p + b * a.O.sb + w.h * a.O.sh + w.i * a.O.sn + c) =
+      u2{pack2<DT>(o.x * inv, o.y * inv), pack2<DT>(o.z * inv, o.w * inv)};
+  if (a.lse && c == 0)
+    a.lse[((size_t)b * a.Hq + w.h) * a.M + w.i] = n > 0 ? (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : -INFINITY;
+}
+
+// The list of the keys that count, one workgroup a batch item: keys in ascending order, those that count first
+__global__ __launch_bounds__(1024) void cross_keys(const uint8_t* mask, int64_t stride, const int32_t* k_len, int N,
+                                                   int32_t* idx, int32_t* count) {
+  __shared__ int wave_on[16];
+  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const uint8_t* mb = mask + b * stride;
+  const int len = k_len ? max(0, min(k_len[b], N)) : N;
+  int32_t* out = idx + (size_t)b * N;
+  // how many count in all
+  int mine = 0;
+  for (int j = tid; j < len; j += 1024) mine += mb[j] != 0;
+  for (int o = 32; o > 0; o >>= 1) mine += __shfl_xor(mine, o, 64);
+  if (lane == 0) wave_on[wave] = mine;
+  __syncthreads();
+  int total = 0;
+  for (int w = 0; w < 16; ++w) total += wave_on[w];
+  if (tid == 0) count[b] = total;
+  int on0 = 0;   // counting keys before this pass
+  for (int j0 = 0; j0 < N; j0 += 1024) {
+    const int j = j0 + tid;
+    const bool on = j < len && mb[j] != 0;
+    const uint64_t bits = __builtin_amdgcn_ballot_w64(on);
+    __syncthreads();
+    if (lane == 0) wave_on[wave] = __popcll(bits);
+    __syncthreads();
+    int before = on0, pass = 0;
+    for (int w = 0; w < 16; ++w) {
+      before += w < wave ? wave_on[w] : 0;
+      pass += wave_on[w];
+    }
+    before += __popcll(bits & ((1ull << lane) - 1));
+    if (j < N) out[on ? before : total + (j - before)] = j;
+    on0 += pass;
+  }
+}
+
+template <int DT, int D>
+hipError_t forward(const CrossArgs& a, hipStream_t s) {
+  const unsigned grid = (unsigned)((int64_t)(a.R + QR - 1) / QR * a.B * a.Hk * a.splits);
+  if (a.splits > 1) {
+    if (a.idx) cross_fwd<DT, D, true, true><<<grid, 64 * NW, 0, s>>>(a);
+    else cross_fwd<DT, D, false, true><<<grid, 64 * NW, 0, s>>>(a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    constexpr int ROWS = 256 / (D / 4);
+    cross_join<DT, D><<<(unsigned)(((int64_t)a.B * a.Hk * a.R + ROWS - 1) / ROWS), 256, 0, s>>>(a);
+  } else {
+    if (a.idx) cross_fwd<DT, D, true, false><<<grid, 64 * NW, 0, s>>>(a);
+    else cross_fwd<DT, D, false, false><<<grid, 64 * NW, 0, s>>>(a);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+}  // namespace cross
+
+hipError_t launch_cross_keys(const uint8_t* k_mask, int64_t stride, const int32_t* k_len, int B, int N, int32_t* idx,
+                             int32_t* count, hipStream_t s) {
+  cross::cross_keys<<<B, 1024, 0, s>>>(k_mask, stride, k_len, N, idx, count);
+  return hipGetLastError();
+}
+
+void cross_plan(CrossArgs& a) {
+  using namespace cross;
+  // keys are split where the rows alone do not give every CU two workgroups
+  const int64_t base = (int64_t)(a.R + QR - 1) / QR * a.B * a.Hk;
+  const int64_t tiles = (a.N + KT - 1) / KT;
+  int64_t splits = base >= 256 ? 1 : (512 + base - 1) / base;
+  if (splits > tiles) splits = tiles;
+  const int64_t per = (tiles + splits - 1) / splits;
+  a.chunk = (int)(per * KT);
+  a.splits = (int)((tiles + per - 1) / per);
+}
+
+hipError_t launch_cross_forward(const CrossArgs& a, hipStream_t s) {
+  if (a.d == 128) return a.dtype == VC_BF16 ? cross::forward<VC_BF16, 128>(a, s) : cross::forward<VC_FP16, 128>(a, s);
+  return a.dtype == VC_BF16 ? cross::forward<VC_BF16, 64>(a, s) : cross::forward<VC_FP16, 64>(a, s);
+}
+
+}  // namespace vc

@@ -100,6 +100,33 @@ struct NormRopeArgs {
   int grid, F, Ht, Wd;   // grid: positions on the latent grid, tables of frames, rows and columns
 };
 
+// A strided tensor of 16-bit rows
+struct Strided {
+  uint16_t* p;
+  int64_t sb, sh, sn;
+};
+
+// Attention of Hq query heads of M queries to Hk = Hq / G key heads of N keys. The query rows of a key head are
+// counted through its G query heads: R = G M rows.
+struct CrossArgs {
+  Strided Q, K, V, O, dO, dQ, dK, dV;
+  int B, Hq, Hk, G, M, N, R, d, dtype;
+  float c;               // score scale times log2(e)
+  float scale;           // score scale
+  const int32_t* k_len;  // [B], or null
+  const int32_t* idx;    // [B][N] the keys that count, in order, then the others; or null
+  const int32_t* count;  // [B] how many count (with idx)
+  float* lse;            // [B][Hq][M] natural logarithm of the softmax's sum
+  // keys split over workgroups: `splits` parts of `chunk` keys, joined from
+  int splits, chunk;
+  float* part_o;         // [splits][B Hk][R][d] unnormalised outputs (backward: parts of dQ)
+  float* part_ml;        // [splits][B Hk][R][2] running maximum (log2 units) and sum
+  // backward
+  float* stats;          // [B Hk][R rounded up to workgroups][2] lse in log2 units and delta
+  int row_splits, row_chunk;   // rows split over workgroups that form dK and dV
+  float* part_kv;        // [row_splits][2][B Hk][N][d] parts of dK and dV
+};
+
 hipError_t launch_prep(const PrepArgs& a, int BH, hipStream_t s);
 ForwardPlan forward_plan(int N, int BH, int qk_fmt, int p_mode);
 hipError_t launch_forward(FwdArgs a, int BH, hipStream_t s);
@@ -110,6 +137,16 @@ hipError_t launch_fp8_score_product(const uint8_t* a, const uint8_t* b, const fl
 hipError_t launch_norm_rope(NormRopeArgs a, hipStream_t s);
 hipError_t launch_norm_rope_backward(NormRopeArgs a, hipStream_t s);
 int norm_rope_parts(int64_t tokens);   // workgroups of the backward kernel
+
+// Which keys count, as a list: idx [B][N], count [B]
+hipError_t launch_cross_keys(const uint8_t* k_mask, int64_t stride, const int32_t* k_len, int B, int N, int32_t* idx,
+                             int32_t* count, hipStream_t s);
+// How a call's keys are split (a.splits, a.chunk), and for the backward pass its rows (a.row_splits, a.row_chunk)
+void cross_plan(CrossArgs& a);
+void cross_plan_backward(CrossArgs& a);
+int64_t cross_stat_rows(int R);
+hipError_t launch_cross_forward(const CrossArgs& a, hipStream_t s);
+hipError_t launch_cross_backward(const CrossArgs& a, hipStream_t s);
 
 // VC_OK, or VC_ERR_HIP with the error kept for vc_last_hip_error
 vc_status hip_status(hipError_t e);

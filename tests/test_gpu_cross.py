@@ -1,0 +1,279 @@
+"""Attention to another sequence and its gradients against the 64-bit form, within the bounds that block_oracle.Cross
+derives from the roundings that the kernels make."""
+import pytest
+
+torch = pytest.importorskip("torch")
+vc = pytest.importorskip("paper_2609_15810_amd")
+import block_oracle as O  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+BF, FP = torch.bfloat16, torch.float16
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    vc.lib()
+
+
+class Problem:
+    """Q, O, dO, dQ as views of token-major tensors, K, V and their gradients of packed ones; guards around outputs"""
+
+    def __init__(self, B, Hq, Hk, M, N, d=128, dtype=BF, mask="none", scale=0.0, packed=True, gain=1.5, seed=0):
+        g = torch.Generator().manual_seed(100 * M + N + seed)
+        self.B, self.Hq, self.Hk, self.M, self.N, self.d, self.dtype = B, Hq, Hk, M, N, d, dtype
+        rand = lambda *s, f=1.0: (torch.randn(s, generator=g) * f).to(dtype)  # noqa: E731
+        q, kv, do = rand(B, M, Hq, d, f=gain), rand(B, N, 2, Hk, d, f=1.2), rand(B, M, Hq, d)
+        self.valid = torch.ones((B, N), dtype=torch.bool)
+        self.kw = {}
+        if mask in ("len", "both"):
+            # from all keys to none; one length beyond the keys
+            k_len = torch.tensor([N + 5 if b == 0 else N * (B - 1 - b) // max(B - 1, 1) for b in range(B)])
+            self.valid &= torch.arange(N)[None] < k_len[:, None]
+            self.kw["k_len"] = k_len.to(torch.int32).cuda()
+        if mask in ("mask", "both"):
+            on = torch.rand((B, N), generator=g) < torch.linspace(0.8, 0.1, B)[:, None]
+            if B > 1:
+                on[-1] = False
+            self.valid &= on
+            self.kw["k_mask"] = on.to(torch.uint8).mul(3).cuda()
+        # what does not count may hold anything
+        kv[~self.valid] = float("nan")
+        self.cpu = [t.transpose(1, 2) for t in (q, kv[:, :, 0], kv[:, :, 1], do)]
+        dev = [t.cuda() for t in (q, kv, do)]
+        self.Q, self.K, self.V = dev[0].transpose(1, 2), dev[1][:, :, 0].transpose(1, 2), dev[1][:, :, 1].transpose(1, 2)
+        self.dO = dev[2].transpose(1, 2)
+        if not packed:
+            self.Q, self.K, self.V, self.dO = (t.contiguous() for t in (self.Q, self.K, self.V, self.dO))
+        self.scale = scale
+        self.op = vc.CrossAttention(B, Hq, Hk, M, N, d, dtype=dtype, sm_scale=scale, masked="k_mask" in self.kw,
+                                    training=True)
+
+    def guarded(self, B, H, n):
+        """[B, H, n, d] inside a wider token-major buffer of sevens, and a check that the rest stayed"""
+        buf = torch.full((B, n + 3, H + 1, self.d), 7.0, dtype=self.dtype, device="cuda")
+        view = buf[:, 1:n + 1, :H].transpose(1, 2)
+
+        def intact():
+            keep = torch.ones_like(buf, dtype=torch.bool)
+            keep[:, 1:n + 1, :H] = False
+            return bool((buf[keep] == 7.0).all())
+        return view, intact
+
+    def forward(self, **kw):
+        out, intact = self.guarded(self.B, self.Hq, self.M)
+        lse = torch.full((self.B, self.Hq, self.M), float("nan"), device="cuda")
+        self.op.forward(self.Q, self.K, self.V, out, lse, **self.kw, **kw)
+        torch.cuda.synchronize()
+        assert intact()
+        return out, lse
+
+    def backward(self, out, lse, **kw):
+        made = [self.guarded(self.B, H, n) for H, n in ((self.Hq, self.M), (self.Hk, self.N), (self.Hk, self.N))]
+        grads = [m[0] for m in made]
+        self.op.backward(self.Q, self.K, self.V, out, lse, self.dO, *grads, **self.kw, **kw)
+        torch.cuda.synchronize()
+        assert all(m[1]() for m in made)
+        return grads
+
+    def check(self, backward=True):
+        out, lse = self.forward()
+        q, k, v, do = self.cpu
+        ref = O.Cross(q, k, v, self.valid, self.dtype, self.scale, do if backward else None)
+        near(out, ref.O, ref.O_err, "O")
+        lse = lse.cpu().double()
+        empty = ref.lse == -float("inf")
+        assert torch.equal(lse == -float("inf"), empty)
+        assert ((lse - ref.lse)[~empty].abs() <= ref.lse_err.expand_as(lse)[~empty]).all()
+        if backward:
+            for name, got in zip(("dQ", "dK", "dV"), self.backward(out, lse.float().cuda())):
+                near(got, getattr(ref, name), getattr(ref, name + "_err"), name)
+
+
+def near(got, ref, err, name):
+    got = got.cpu().double()
+    assert got.isfinite().all(), name
+    bad = (got - ref).abs() > err
+    assert not bad.any(), (name, int(bad.sum()), float(((got - ref).abs() / err.clamp(min=1e-300)).max()))
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("d", [128, 64])
+@pytest.mark.parametrize("mask", ["none", "len", "mask", "both"])
+@pytest.mark.parametrize("B,Hq,Hk,M,N", [(3, 4, 2, 130, 100), (2, 3, 3, 33, 257)])
+def test_formats(dtype, d, mask, B, Hq, Hk, M, N):
+    Problem(B, Hq, Hk, M, N, d, dtype, mask).check()
+
+
+@pytest.mark.parametrize("packed", [True, False])
+@pytest.mark.parametrize("B,Hq,Hk,M,N", [
+    (1, 1, 1, 1, 1), (2, 2, 1, 1, 2), (1, 1, 1, 700, 1), (1, 2, 2, 1, 700),          # one query, one key
+    (1, 2, 2, 31, 63), (1, 2, 2, 32, 64), (1, 2, 2, 33, 65), (1, 2, 2, 128, 128), (1, 1, 1, 129, 129),   # tile edges
+    (1, 8, 1, 5, 40), (2, 7, 1, 37, 300), (1, 40, 40, 3, 20),                        # groups of heads
+    (1, 1, 1, 3001, 77), (16, 2, 2, 200, 64)])
+def test_sizes(packed, B, Hq, Hk, M, N):
+    Problem(B, Hq, Hk, M, N, packed=packed).check()
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("B,Hq,Hk,M,N,mask", [(1, 8, 2, 1, 3000, "none"), (2, 4, 4, 40, 4100, "mask"),
+                                              (3, 2, 1, 16, 2500, "len"), (1, 32, 8, 1, 1500, "both")])
+def test_split_keys(dtype, B, Hq, Hk, M, N, mask):
+    Problem(B, Hq, Hk, M, N, 128, dtype, mask).check()
+
+
+@pytest.mark.parametrize("d", [128, 64])
+def test_split_rows(d):
+    Problem(1, 2, 1, 4001, 130, d).check()
+    Problem(2, 2, 2, 2100, 40, d, mask="mask").check()
+
+
+def test_many_rows_at_once():
+    """the whole grid of a call of several thousand workgroups, on sampled rows"""
+    p = Problem(1, 12, 12, 32760, 512)
+    out, lse = p.forward()
+    at = torch.cat([torch.arange(200), torch.arange(16300, 16500), torch.arange(32560, 32760)])
+    q, k, v, _ = p.cpu
+    ref = O.Cross(q[:, :, at], k, v, p.valid, BF)
+    near(out[:, :, at.cuda()], ref.O, ref.O_err, "O")
+
+
+@pytest.mark.parametrize("scale", [0.02, 0.5])
+def test_scale(scale):
+    Problem(1, 2, 2, 50, 90, scale=scale).check()
+
+
+def test_peaked_rows():
+    # scores of several hundred: the softmax takes one key, the running maximum moves over the tiles
+    Problem(1, 2, 2, 70, 400, gain=60.0).check(backward=False)
+
+
+def test_shared_operands():
+    # one set of encoder states for all items, one row of queries for all places
+    p = Problem(3, 2, 2, 40, 70)
+    p.K, p.V = p.K[:1].expand(3, 2, 70, 128), p.V[:1].expand(3, 2, 70, 128)
+    p.Q = p.Q[:, :, :1].expand(3, 2, 40, 128)
+    q, k, v, do = p.cpu
+    p.cpu = [q[:, :, :1].expand(3, 2, 40, 128), k[:1].expand(3, 2, 70, 128), v[:1].expand(3, 2, 70, 128), do]
+    p.check()
+
+
+def test_offsets_beyond_32_bits():
+    p = Problem(1, 1, 1, 40, 5)
+    far = torch.empty(4 * (1 << 30) + 128, dtype=BF, device="cuda")   # rows 2 GiB apart
+    k = far.as_strided((1, 1, 5, 128), (8, 8, 1 << 30, 1))
+    k.copy_(p.K)
+    p.K = k
+    p.check()
+    out = far.as_strided((1, 1, 5, 128), (8, 8, 1 << 30, 1))
+    q5 = p.Q[:, :, :5]
+    op = vc.CrossAttention(1, 1, 1, 5, 5)
+    near_o = torch.empty((1, 1, 5, 128), dtype=BF, device="cuda")
+    kk = p.K.contiguous()
+    op.forward(q5, kk, p.V, near_o)
+    op.forward(q5, kk, p.V, out)
+    assert torch.equal(out, near_o)
+
+
+def test_reproducible():
+    p = Problem(2, 4, 2, 1000, 300, mask="mask")
+    out, lse = p.forward()
+    grads = p.backward(out, lse)
+    for _ in range(3):
+        again, lse2 = p.forward()
+        assert torch.equal(again, out) and torch.equal(lse2, lse)
+        assert all(torch.equal(a, b) for a, b in zip(p.backward(out, lse), grads))
+
+
+def test_values_that_are_not_finite():
+    # an infinite value of a key that counts reaches the rows of its head, and nothing else
+    p = Problem(1, 2, 2, 40, 100)
+    clean, _ = p.forward()
+    clean = clean.clone()
+    p.V[0, 1, 99, 5] = float("inf")
+    out, _ = p.forward()
+    assert torch.equal(out[0, 0], clean[0, 0])
+    assert (out[0, 1, :, 5] == float("inf")).all()
+    keep = torch.arange(128, device="cuda") != 5
+    assert torch.equal(out[0, 1][:, keep], clean[0, 1][:, keep])
+    # a NaN in a query spoils its own row
+    p.V[0, 1, 99, 5] = 0.0
+    clean, _ = p.forward()
+    clean = clean.clone()
+    p.Q[0, 0, 7, 3] = float("nan")
+    out, _ = p.forward()
+    assert out[0, 0, 7].isnan().all()
+    rows = torch.arange(40, device="cuda") != 7
+    assert torch.equal(out[:, :, rows], clean[:, :, rows])
+
+
+def test_gradient_against_differences():
+    """sum(O dO) along directions of Q, K and V by central differences of the forward kernel in fp16: each value of O is
+    off by half a step and P's rounding, and the step's third-order part is the cube of its size."""
+    p = Problem(1, 2, 1, 20, 30, 64, FP)
+    out, lse = p.forward()
+    grads = p.backward(out, lse)
+    g = torch.Generator().manual_seed(5)
+    for name, grad in zip("QKV", grads):
+        x = getattr(p, name)
+        u = torch.randn(x.shape, generator=g).cuda()
+        u /= u.square().mean().sqrt()
+        h, loss, at, size = 0.06, [], [], 0.0
+        for s in (1.0, -1.0):
+            setattr(p, name, (x + s * h * u).to(FP))
+            at.append(getattr(p, name).double())
+            o = p.forward()[0].double()
+            loss.append((o * p.dO.double()).sum())
+            size = max(size, float((o * p.dO.double()).abs().sum()))
+        setattr(p, name, x)
+        got, want = float((grad.double() * (at[0] - at[1])).sum()), float(loss[0] - loss[1])
+        # scores move by up to h |k| ~ 0.06 * 1.2 * 4 sigma: a third-order part of (0.3)^3 / 6 of the size
+        assert abs(got - want) <= size * (4 * 2.0 ** -11 + 0.3 ** 3 / 6), (name, got, want, size)
+
+
+def test_streams_and_graph():
+    p = Problem(2, 4, 2, 300, 200, mask="mask")
+    out, lse = p.forward()
+    grads = p.backward(out, lse)
+    want = [t.clone() for t in [out, lse] + grads]
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        a = p.forward()
+    assert torch.equal(a[0], want[0])
+    b = p.backward(*p.forward(stream=s), stream=s)
+    assert all(torch.equal(x, y) for x, y in zip(b, want[2:]))
+    other = Problem(1, 2, 2, 900, 700)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        p.op.forward(p.Q, p.K, p.V, out, lse, **p.kw)
+        p.op.backward(p.Q, p.K, p.V, out, lse, p.dO, *grads, **p.kw)
+    for _ in range(3):
+        for t in [out, lse] + grads:
+            t.zero_()
+        other.backward(*other.forward())
+        torch.cuda.synchronize()
+        g.replay()
+        other.backward(*other.forward())
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip([out, lse] + grads, want))
+
+
+def test_wrong_tensors_refused():
+    p = Problem(1, 4, 2, 33, 20)
+    out = torch.empty((1, 4, 33, 128), dtype=BF, device="cuda")
+    for q in (p.Q.cpu(), p.Q.half(), p.Q[:, :3], p.Q[:, :, :, :64], p.Q.transpose(2, 3).contiguous().transpose(2, 3)):
+        with pytest.raises(vc.VcError):
+            p.op.forward(q, p.K, p.V, out)
+    with pytest.raises(vc.VcError):
+        p.op.forward(p.Q, p.K, p.V, out, k_len=torch.ones(1, dtype=torch.int64, device="cuda"))
+    with pytest.raises(vc.VcError):
+        p.op.forward(p.Q, p.K, p.V, out, k_mask=torch.ones((1, 20), dtype=torch.uint8, device="cuda"))   # not masked
+    with pytest.raises(vc.VcError):
+        p.op.forward(p.Q, p.K, p.V, out[:, :, :1].expand(1, 4, 33, 128))
+    op = vc.CrossAttention(1, 4, 2, 33, 20, masked=True)
+    with pytest.raises(vc.VcError):
+        op.forward(p.Q, p.K, p.V, out)   # masked, without a mask
