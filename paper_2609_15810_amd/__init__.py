@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from dataclasses import dataclass
 
 import numpy as np
@@ -61,6 +62,10 @@ class Prepped(C.Structure):
 
 class View(C.Structure):
     _fields_ = [("data", C.c_void_p), ("sb", C.c_int64), ("sh", C.c_int64), ("sn", C.c_int64)]
+
+
+_VIEW = C.c_char_p              # a view argument: the bytes of a View (made faster than the structure), or None
+_pack_view = struct.Struct("4q").pack
 
 
 class CrossShape(C.Structure):
@@ -123,21 +128,18 @@ def lib():
         L.vc_fp8_score_product.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p]
         L.vc_cross_attn_workspace_size.restype = C.c_size_t
         L.vc_cross_attn_workspace_size.argtypes = [C.POINTER(CrossShape), C.POINTER(CrossOpts), C.c_int32]
-        inputs = [C.POINTER(CrossShape), C.POINTER(CrossOpts)] + [C.POINTER(View)] * 3 + \
-            [C.c_void_p, C.c_void_p, C.c_int64, C.POINTER(View), C.c_void_p]
+        p = C.c_void_p
         L.vc_cross_attn_forward.restype = C.c_int
-        L.vc_cross_attn_forward.argtypes = inputs + [C.c_void_p, C.c_size_t, C.c_void_p]
+        L.vc_cross_attn_forward.argtypes = [p, p] + [_VIEW] * 3 + [p, p, C.c_int64, _VIEW, p] + [p, C.c_size_t, p]
         L.vc_cross_attn_backward.restype = C.c_int
-        L.vc_cross_attn_backward.argtypes = inputs + [C.POINTER(View)] * 4 + [C.c_void_p, C.c_size_t, C.c_void_p]
-        L.vc_norm_rope.restype = C.c_int
-        L.vc_norm_rope.argtypes = [C.POINTER(NormRopeShape), C.POINTER(NormRopeOpts)] + [C.POINTER(View)] * 2 + \
-            [C.c_void_p] * 5 + [C.POINTER(View)] * 2 + [C.c_void_p]
+        L.vc_cross_attn_backward.argtypes = [p, p] + [_VIEW] * 3 + [p, p, C.c_int64, _VIEW, p] + [_VIEW] * 4 + \
+            [p, C.c_size_t, p]
         L.vc_norm_rope_workspace_size.restype = C.c_size_t
         L.vc_norm_rope_workspace_size.argtypes = [C.POINTER(NormRopeShape), C.POINTER(NormRopeOpts)]
+        L.vc_norm_rope.restype = C.c_int
+        L.vc_norm_rope.argtypes = [p, p] + [_VIEW] * 2 + [p] * 5 + [_VIEW] * 2 + [p]
         L.vc_norm_rope_backward.restype = C.c_int
-        L.vc_norm_rope_backward.argtypes = [C.POINTER(NormRopeShape), C.POINTER(NormRopeOpts)] + \
-            [C.POINTER(View)] * 2 + [C.c_void_p] * 5 + [C.POINTER(View)] * 4 + \
-            [C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.vc_norm_rope_backward.argtypes = [p, p] + [_VIEW] * 2 + [p] * 5 + [_VIEW] * 4 + [p, p, p, C.c_size_t, p]
         L.vc_rope_line_tables.restype = C.c_int
         L.vc_rope_line_tables.argtypes = [C.c_int32, C.c_int32, C.c_double, C.POINTER(RopeScaling), C.c_void_p,
                                           C.c_void_p]
@@ -344,37 +346,6 @@ def rope_line_tables_host(rows: int, rot: int = D, theta: float = 10000.0, scali
     return cos_t, sin_t
 
 
-class _Operands:
-    """Marshalling of one operator's tensors: checks each against its shape, type and device (the library sees
-    addresses only) and makes the C arguments. Raises VcError as the library would."""
-
-    def __init__(self, fn, dtype, device):
-        self.fn, self.dtype, self.device = fn, dtype, device
-
-    def refuse(self, status):
-        raise VcError(self.fn, status, lib())
-
-    def view(self, t, shape):
-        if t is None:
-            return None
-        if tuple(t.shape) != shape or t.dtype != self.dtype or t.device != self.device:
-            self.refuse(2)
-        sb, sh, sn, sc = t.stride()
-        if sc != 1:
-            self.refuse(5)
-        return C.byref(View(t.data_ptr(), sb, sh, sn))
-
-    def flat(self, t, shape, dtype):
-        """address of a contiguous tensor (shape None: of any)"""
-        if t is None:
-            return None
-        if (shape is not None and tuple(t.shape) != shape) or t.dtype != dtype or t.device != self.device:
-            self.refuse(2)
-        if not t.is_contiguous():
-            self.refuse(5)
-        return t.data_ptr()
-
-
 def _device(device):
     import torch
     d = torch.device(device)
@@ -382,8 +353,9 @@ def _device(device):
 
 
 class _Operator:
-    """What the operators around the attention have in common: a call runs on the device of its tensors, on the
-    given stream or that device's current one."""
+    """What the operators around the attention have in common. Each tensor is checked against its shape, type and
+    device (the library sees addresses only); VcError is raised as for a refusal of the library. A call runs on the
+    device of its tensors, on the given stream or that device's current one."""
 
     def __init__(self, dtype, device):
         import torch
@@ -393,17 +365,44 @@ class _Operator:
         self.dtype, self.device = dtype, _device(device)
         self.c_dtype = types[dtype]
         self.ws = None
+        self._f32, self._i32 = torch.float32, torch.int32
+        self._current_device, self._current_stream = torch.cuda.current_device, torch._C._cuda_getCurrentRawStream
+
+    def _refuse(self, status):
+        raise VcError(type(self).__name__, status, lib())
+
+    def _view(self, t, shape):
+        """a tensor in any strides whose channels are contiguous"""
+        if t is None:
+            return None
+        if t.shape != shape or t.dtype != self.dtype or t.device != self.device:
+            self._refuse(2)
+        sb, sh, sn, sc = t.stride()
+        if sc != 1:
+            self._refuse(5)
+        return _pack_view(t.data_ptr(), sb, sh, sn)
+
+    def _flat(self, t, shape, dtype):
+        """a contiguous tensor"""
+        if t is None:
+            return None
+        if t.shape != shape or t.dtype != dtype or t.device != self.device:
+            self._refuse(2)
+        if not t.is_contiguous():
+            self._refuse(5)
+        return t.data_ptr()
 
     def _call(self, fn, stream, *args):
-        import torch
-        s = torch.cuda.current_stream(self.device) if stream is None else stream
-        L = getattr(lib(), fn)
-        if torch.cuda.current_device() == self.device.index:
-            st = L(*args, s.cuda_stream)
+        index = self.device.index
+        s = self._current_stream(index) if stream is None else stream.cuda_stream
+        if self._current_device() == index:
+            st = getattr(lib(), fn)(*args, s)
         else:
+            import torch
             with torch.cuda.device(self.device):
-                st = L(*args, s.cuda_stream)
-        _check(fn, st)
+                st = getattr(lib(), fn)(*args, s)
+        if st != VC_OK:
+            raise VcError(fn, st, lib())
 
 
 class NormRope(_Operator):
@@ -420,51 +419,54 @@ class NormRope(_Operator):
         import torch
         super().__init__(torch.bfloat16 if dtype is None else dtype, device)
         self.shape = NormRopeShape(B, Hq, Hk, N, d)
-        rot = 0 if layout == ROPE_NONE else (d if rot is None else rot)
+        self.rot = 0 if layout == ROPE_NONE else (d if rot is None else rot)
         # the tables' rows are known with the tables; 1 stands for them in the checks here
-        self.opts = NormRopeOpts(self.c_dtype, norm, layout, rot, eps, 1, *(grid or (0, 0, 0)))
+        self.opts = self._opts(norm, layout, eps, 1, grid)
         size = lib().vc_norm_rope_workspace_size(C.byref(self.shape), C.byref(self.opts))
         if size == C.c_size_t(-1).value:
             raise VcError("vc_norm_rope_workspace_size", 2, lib())
         if training:
             self.ws = torch.empty(max(size, 16), dtype=torch.uint8, device=self.device)
-        self._sizes = (B, Hq, N, d), (B, Hk, N, d)
+        self._q, self._k = (B, Hq, N, d), (B, Hk, N, d)
+        span = (lambda H: (H * d,)) if norm == NORM_TOKEN else (lambda H: (d,))
+        self._qw, self._kw, self._pos = span(Hq), span(Hk), (B, N)
+        self._norm, self._layout, self._eps, self._grid = norm, layout, eps, grid
+        self._c_shape = C.byref(self.shape)
 
-    def _common(self, fn, q, k, q_weight, k_weight, cos, sin, pos):
-        import torch
-        x, (sq, sk), o = _Operands(fn, self.dtype, self.device), self._sizes, self.opts
-        if (k is not None or k_weight is not None) and sk[1] == 0:
-            x.refuse(2)
-        if o.layout != ROPE_NONE:
+    def _opts(self, norm, layout, eps, rows, grid):
+        return NormRopeOpts(self.c_dtype, norm, layout, self.rot, eps, rows, *(grid or (0, 0, 0)))
+
+    def _inputs(self, q, k, q_weight, k_weight, cos, sin, pos):
+        if self.shape.Hk == 0 and (k is not None or k_weight is not None):
+            self._refuse(2)
+        opts = self.opts
+        if self._layout != ROPE_NONE:
             if cos is None or sin is None:
-                x.refuse(1)
-            rows = o.F + o.Ht + o.Wd if o.F else len(cos)
-            shape = (rows, o.rot // 2)
-            cos, sin = x.flat(cos, shape, torch.float32), x.flat(sin, shape, torch.float32)
-            o.rows = rows
+                self._refuse(1)
+            rows = sum(self._grid) if self._grid else len(cos)
+            table = (rows, self.rot // 2)
+            cos, sin = self._flat(cos, table, self._f32), self._flat(sin, table, self._f32)
+            if not self._grid:
+                opts = self._opts(self._norm, self._layout, self._eps, rows, None)
         else:
             cos = sin = None
-        span = (lambda s: (s[1] * s[3],)) if o.norm == NORM_TOKEN else (lambda s: (s[3],))
-        return x, span, (C.byref(self.shape), C.byref(o), x.view(q, sq), x.view(k, sk),
-                         x.flat(q_weight, span(sq), torch.float32), x.flat(k_weight, span(sk), torch.float32), cos, sin,
-                         x.flat(pos, (sq[0], sq[2]), torch.int32))
+        return (self._c_shape, C.byref(opts), self._view(q, self._q), self._view(k, self._k),
+                self._flat(q_weight, self._qw, self._f32), self._flat(k_weight, self._kw, self._f32), cos, sin,
+                self._flat(pos, self._pos, self._i32))
 
     def forward(self, q, k, q_out, k_out, q_weight=None, k_weight=None, cos=None, sin=None, pos=None, stream=None):
         """q_out, k_out = the normed and turned q, k (k and k_out None with Hk = 0)."""
-        x, _, args = self._common("vc_norm_rope", q, k, q_weight, k_weight, cos, sin, pos)
-        sq, sk = self._sizes
-        self._call("vc_norm_rope", stream, *args, x.view(q_out, sq), x.view(k_out, sk))
+        self._call("vc_norm_rope", stream, *self._inputs(q, k, q_weight, k_weight, cos, sin, pos),
+                   self._view(q_out, self._q), self._view(k_out, self._k))
 
     def backward(self, q, k, dq_out, dk_out, dq, dk, q_weight=None, k_weight=None, dq_weight=None, dk_weight=None,
                  cos=None, sin=None, pos=None, stream=None):
         """dq, dk (and dq_weight, dk_weight where given) = the gradients of q, k and of the weights."""
-        import torch
-        fn = "vc_norm_rope_backward"
-        x, span, args = self._common(fn, q, k, q_weight, k_weight, cos, sin, pos)
-        sq, sk = self._sizes
-        self._call(fn, stream, *args, x.view(dq_out, sq), x.view(dk_out, sk), x.view(dq, sq), x.view(dk, sk),
-                   x.flat(dq_weight, span(sq), torch.float32), x.flat(dk_weight, span(sk), torch.float32),
-                   None if self.ws is None else self.ws.data_ptr(), 0 if self.ws is None else self.ws.numel())
+        self._call("vc_norm_rope_backward", stream, *self._inputs(q, k, q_weight, k_weight, cos, sin, pos),
+                   self._view(dq_out, self._q), self._view(dk_out, self._k), self._view(dq, self._q),
+                   self._view(dk, self._k), self._flat(dq_weight, self._qw, self._f32),
+                   self._flat(dk_weight, self._kw, self._f32), None if self.ws is None else self.ws.data_ptr(),
+                   0 if self.ws is None else self.ws.numel())
 
 
 class CrossAttention(_Operator):
@@ -481,38 +483,37 @@ class CrossAttention(_Operator):
         super().__init__(torch.bfloat16 if dtype is None else dtype, device)
         self.shape = CrossShape(B, Hq, Hk, M, N, d)
         self.opts = CrossOpts(self.c_dtype, sm_scale, int(bool(masked)))
+        self._c = C.byref(self.shape), C.byref(self.opts)
         size = 0
         for backward in range(2 if training else 1):
-            need = lib().vc_cross_attn_workspace_size(C.byref(self.shape), C.byref(self.opts), backward)
+            need = lib().vc_cross_attn_workspace_size(*self._c, backward)
             if need == C.c_size_t(-1).value:
                 raise VcError("vc_cross_attn_workspace_size", 2, lib())
             size = max(size, need)
-        self.training = bool(training)
         self.ws = torch.empty(max(size, 16), dtype=torch.uint8, device=self.device)
-        self._q, self._k = (B, Hq, M, d), (B, Hk, N, d)
+        self._ws = self.ws.data_ptr(), self.ws.numel()
+        self._q, self._k, self._b, self._mask, self._lse = (B, Hq, M, d), (B, Hk, N, d), (B,), (B, N), (B, Hq, M)
+        self._mask_types = (torch.uint8, torch.bool)
 
-    def _inputs(self, fn, Q, K, V, k_len, k_mask, O, lse):
-        import torch
-        x, (B, Hq, M, _), N = _Operands(fn, self.dtype, self.device), self._q, self._k[2]
-        stride = 0
+    def _inputs(self, Q, K, V, k_len, k_mask, O, lse):
+        mask, stride = None, 0
         if k_mask is not None:
-            if tuple(k_mask.shape) != (B, N) or k_mask.dtype not in (torch.uint8, torch.bool) or \
-                    k_mask.device != self.device:
-                x.refuse(2)
-            if k_mask.stride(1) != 1 and N > 1:
-                x.refuse(5)
-            stride = k_mask.stride(0)
-        return x, (C.byref(self.shape), C.byref(self.opts), x.view(Q, self._q), x.view(K, self._k), x.view(V, self._k),
-                   x.flat(k_len, (B,), torch.int32), None if k_mask is None else k_mask.data_ptr(), stride,
-                   x.view(O, self._q), x.flat(lse, (B, Hq, M), torch.float32))
+            if k_mask.shape != self._mask or k_mask.dtype not in self._mask_types or k_mask.device != self.device:
+                self._refuse(2)
+            stride, s = k_mask.stride()
+            if s != 1 and self.shape.N > 1:
+                self._refuse(5)
+            mask = k_mask.data_ptr()
+        return (*self._c, self._view(Q, self._q), self._view(K, self._k), self._view(V, self._k),
+                self._flat(k_len, self._b, self._i32), mask, stride, self._view(O, self._q),
+                self._flat(lse, self._lse, self._f32))
 
     def forward(self, Q, K, V, O, lse=None, k_len=None, k_mask=None, stream=None):
         """O = softmax(sm_scale Q K^T) V; lse [B, Hq, M] fp32 is written where given (for backward)."""
-        _, args = self._inputs("vc_cross_attn_forward", Q, K, V, k_len, k_mask, O, lse)
-        self._call("vc_cross_attn_forward", stream, *args, self.ws.data_ptr(), self.ws.numel())
+        self._call("vc_cross_attn_forward", stream, *self._inputs(Q, K, V, k_len, k_mask, O, lse), *self._ws)
 
     def backward(self, Q, K, V, O, lse, dO, dQ, dK, dV, k_len=None, k_mask=None, stream=None):
-        """dQ, dK, dV from dO, with O and lse as forward() wrote them."""
-        x, args = self._inputs("vc_cross_attn_backward", Q, K, V, k_len, k_mask, O, lse)
-        self._call("vc_cross_attn_backward", stream, *args, x.view(dO, self._q), x.view(dQ, self._q),
-                   x.view(dK, self._k), x.view(dV, self._k), self.ws.data_ptr(), self.ws.numel())
+        """dQ, dK, dV from dO, with O and lse as forward() wrote them (training=True)."""
+        self._call("vc_cross_attn_backward", stream, *self._inputs(Q, K, V, k_len, k_mask, O, lse),
+                   self._view(dO, self._q), self._view(dQ, self._q), self._view(dK, self._k), self._view(dV, self._k),
+                   *self._ws)

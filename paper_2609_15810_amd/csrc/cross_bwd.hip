@@ -346,18 +346,36 @@ __global__ __launch_bounds__(64 * NW, 1) void cross_dkv(CrossArgs a) {
   store_rows<DT, D>(dv, 1.f, lds, lane, [&](int r) __attribute__((always_inline)) { return row_of(a.dV, r); });
 }
 
-// dQ from the parts of split keys: d / 4 lanes a row
-template <int DT, int D>
-__global__ __launch_bounds__(256) void cross_join_dq(CrossArgs a) {
-  constexpr int L = D / 4, ROWS = 256 / L;
-  const int64_t rows = (int64_t)a.B * a.Hk * a.R, at = (int64_t)blockIdx.x * ROWS + threadIdx.x / L;
-  if (at >= rows) return;
-  const int c = threadIdx.x % L * 4;
+// Sums of parts [part][row][D] at p (rows * D apart by `step`): as cross_join, d / 4 lanes and `groups` of them a row;
+// the sum is complete in the lanes of group 0
+template <int D>
+__device__ __forceinline__ float4 join_parts(const float* p, size_t step, int parts, int groups, bool in) {
+  constexpr int L = D / 4, ALL = 256 / L;
+  __shared__ __attribute__((aligned(16))) float so[ALL][D];
+  const int slot = threadIdx.x / L, g = slot & (groups - 1), c = threadIdx.x % L * 4;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int s = 0; s < a.splits; ++s) {
-    const float4 v = *reinterpret_cast<const float4*>(a.part_o + (s * rows + at) * D + c);
-    o.x += v.x, o.y += v.y, o.z += v.z, o.w += v.w;
+  auto add = [&](float4 v) __attribute__((always_inline)) { o.x += v.x, o.y += v.y, o.z += v.z, o.w += v.w; };
+  if (in) {
+#pragma unroll 4
+    for (int s = g; s < parts; s += groups) add(*reinterpret_cast<const float4*>(p + s * step + c));
   }
+  if (groups > 1) {
+    *reinterpret_cast<float4*>(&so[slot][c]) = o;
+    __syncthreads();
+    if (g == 0)
+      for (int i = 1; i < groups; ++i) add(*reinterpret_cast<const float4*>(&so[slot + i][c]));
+  }
+  return o;
+}
+
+// dQ from the parts of split keys
+template <int DT, int D>
+__global__ __launch_bounds__(256) void cross_join_dq(CrossArgs a, int groups) {
+  constexpr int L = D / 4, ALL = 256 / L;
+  const int slot = threadIdx.x / L, c = threadIdx.x % L * 4;
+  const int64_t rows = (int64_t)a.B * a.Hk * a.R, at = (int64_t)blockIdx.x * (ALL / groups) + slot / groups;
+  const float4 o = join_parts<D>(a.part_o + at * D, rows * D, a.splits, groups, at < rows);
+  if ((slot & (groups - 1)) != 0 || at >= rows) return;
   const uint32_t bh = at / a.R;
   const int b = bh / (uint32_t)a.Hk, hk = bh - b * a.Hk;
   const QueryRow w = query_row(a, hk, (int)(at - (int64_t)bh * a.R));
@@ -368,19 +386,16 @@ __global__ __launch_bounds__(256) void cross_join_dq(CrossArgs a) {
 
 // dK and dV from the parts of split rows; zeros for keys that do not count
 template <int DT, int D>
-__global__ __launch_bounds__(256) void cross_join_dkv(CrossArgs a) {
-  constexpr int L = D / 4, ROWS = 256 / L;
-  const int64_t keys = (int64_t)a.B * a.Hk * a.N, at = (int64_t)blockIdx.x * ROWS + threadIdx.x / L;
-  if (at >= keys) return;
-  const int c = threadIdx.x % L * 4, which = blockIdx.y;
-  const uint32_t bh = at / a.N;
-  const int b = bh / (uint32_t)a.Hk, hk = bh - b * a.Hk, j = (int)(at - (int64_t)bh * a.N);
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (j < keys_of(a, b))
-    for (int s = 0; s < a.row_splits; ++s) {
-      const float4 v = *reinterpret_cast<const float4*>(a.part_kv + ((2 * s + which) * keys + at) * D + c);
-      o.x += v.x, o.y += v.y, o.z += v.z, o.w += v.w;
-    }
+__global__ __launch_bounds__(256) void cross_join_dkv(CrossArgs a, int groups) {
+  constexpr int L = D / 4, ALL = 256 / L;
+  const int slot = threadIdx.x / L, c = threadIdx.x % L * 4, which = blockIdx.y;
+  const int64_t keys = (int64_t)a.B * a.Hk * a.N, at = (int64_t)blockIdx.x * (ALL / groups) + slot / groups;
+  const bool in = at < keys;
+  const uint32_t bh = (in ? at : 0) / a.N;
+  const int b = bh / (uint32_t)a.Hk, hk = bh - b * a.Hk, j = in ? (int)(at - (int64_t)bh * a.N) : 0;
+  const float4 o = join_parts<D>(a.part_kv + (which * keys + at) * D, 2 * keys * D, a.row_splits, groups,
+                                 in && j < keys_of(a, b));
+  if ((slot & (groups - 1)) != 0 || !in) return;
   const float f = which ? 1.f : a.scale;
   const Strided& t = which ? a.dV : a.dK;
   const int64_t i = a.idx ? a.idx[(size_t)b * a.N + j] : j;
@@ -390,7 +405,8 @@ __global__ __launch_bounds__(256) void cross_join_dkv(CrossArgs a) {
 
 template <int DT, int D>
 hipError_t backward(const CrossArgs& a, hipStream_t s) {
-  constexpr int ROWS = 256 / (D / 4);
+  const int gj = join_groups(a.splits), gkj = join_groups(a.row_splits);
+  const int64_t jq = 256 / (D / 4) / gj, jk = 256 / (D / 4) / gkj;   // joined rows of a workgroup
   const int64_t heads = (int64_t)a.B * a.Hk;
   const unsigned gq = (unsigned)((int64_t)(a.R + QR - 1) / QR * heads * a.splits);
   const unsigned gk = (unsigned)((int64_t)(a.N + KB - 1) / KB * heads * a.row_splits);
@@ -399,7 +415,7 @@ hipError_t backward(const CrossArgs& a, hipStream_t s) {
     if (a.idx) cross_dq<DT, D, true, true><<<gq, 64 * NW, 0, s>>>(a);
     else cross_dq<DT, D, false, true><<<gq, 64 * NW, 0, s>>>(a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    cross_join_dq<DT, D><<<(unsigned)((heads * a.R + ROWS - 1) / ROWS), 256, 0, s>>>(a);
+    cross_join_dq<DT, D><<<(unsigned)((heads * a.R + jq - 1) / jq), 256, 0, s>>>(a, gj);
   } else {
     if (a.idx) cross_dq<DT, D, true, false><<<gq, 64 * NW, 0, s>>>(a);
     else cross_dq<DT, D, false, false><<<gq, 64 * NW, 0, s>>>(a);
@@ -408,7 +424,7 @@ hipError_t backward(const CrossArgs& a, hipStream_t s) {
   if (a.row_splits > 1) {
     cross_dkv<DT, D, true><<<gk, 64 * NW, 0, s>>>(a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    cross_join_dkv<DT, D><<<dim3((unsigned)((heads * a.N + ROWS - 1) / ROWS), 2), 256, 0, s>>>(a);
+    cross_join_dkv<DT, D><<<dim3((unsigned)((heads * a.N + jk - 1) / jk), 2), 256, 0, s>>>(a, gkj);
   } else {
     cross_dkv<DT, D, false><<<gk, 64 * NW, 0, s>>>(a);
   }

@@ -23,9 +23,28 @@ __device__ __forceinline__ v16f mma(u4 a, u4 b, v16f c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f8, a), __builtin_bit_cast(f8, b), c, 0, 0, 0);
 }
 
-// exchange with lane l ^ 32 (the other half of a column's results)
-__device__ __forceinline__ float half_sum(float v) { return v + __shfl_xor(v, 32, 64); }
-__device__ __forceinline__ float half_max(float v) { return fmaxf(v, __shfl_xor(v, 32, 64)); }
+// Empty asm that reads and rewrites x: what the compiler knows of x's value ends here
+template <typename V>
+__device__ __forceinline__ void pin(V& x) {
+  asm volatile("" : "+v"(x));
+}
+
+// sum and maximum of v over lanes l and l ^ 32 (the other half of a column's results). The swap's two results are both
+// halves' values; they are pinned, since a maximum over them has been compiled into one over a single one.
+__device__ __forceinline__ float half_sum(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  uint32_t x = r[0], y = r[1];
+  pin(x);
+  pin(y);
+  return __uint_as_float(x) + __uint_as_float(y);
+}
+__device__ __forceinline__ float half_max(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  uint32_t x = r[0], y = r[1];
+  pin(x);
+  pin(y);
+  return fmaxf(__uint_as_float(x), __uint_as_float(y));
+}
 
 // Tiles of rows of D 16-bit values in LDS, without padding: the 16-byte piece `ch` of row `r` stands in place
 // ch ^ key(r), so that the pieces that 16 lanes read from 16 consecutive rows lie in different banks.
@@ -65,6 +84,37 @@ __device__ __forceinline__ void copy16(const void* src, const void* lds) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "s"(to) : "memory", "m0");
 }
 
+// The copies of a tile of ROWS rows at a constant stride (in elements, below FAR_STRIDE) by the NW waves of a workgroup,
+// through a buffer descriptor: a lane's offset from the tile's first row is the same for all tiles, and rows behind
+// the `valid` first are out of the buffer's range, which reads as zero without an access.
+constexpr int64_t FAR_STRIDE = 1 << 24;   // 64 rows of less than this stay below 2^32 bytes
+template <int D, int ROWS, int NW>
+struct Copier {
+  using T = Tile<D>;
+  static constexpr int COPIES = ROWS / T::ROWS_PER_COPY / NW;
+  uint32_t off, step, row_bytes;
+  __device__ __forceinline__ Copier(int64_t stride, int wave, int lane) {
+    const int r = wave * T::ROWS_PER_COPY + lane / T::CH;   // the places of its other rows have the same key
+    row_bytes = 2 * (uint32_t)stride;
+    off = r * row_bytes + 16 * ((lane % T::CH) ^ T::key(r));
+    step = NW * T::ROWS_PER_COPY * row_bytes;
+  }
+  // tile: address of the tile's first row, the same for all lanes
+  __device__ __forceinline__ void copy(const uint16_t* tile, int valid, const uint8_t* lds, int wave) const {
+    typedef int v4i __attribute__((ext_vector_type(4)));
+    const uint64_t p = reinterpret_cast<uint64_t>(tile);
+    const uint32_t bytes = valid > 0 ? (min(valid, ROWS) - 1) * row_bytes + T::ROW : 0u;
+    const v4i rsrc = {(int)(uint32_t)p, (int)(uint32_t)(p >> 32), (int)bytes, 0x00020000};
+    const uint32_t to = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const void*)lds)) +
+                        wave * 1024;
+#pragma unroll
+    for (int u = 0; u < COPIES; ++u)
+      asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(off + u * step), "s"(rsrc),
+                   "s"(__builtin_amdgcn_readfirstlane(to + u * NW * 1024))
+                   : "memory", "m0");
+  }
+};
+
 // all of this wave's memory operations are done
 __device__ __forceinline__ void wait_copies() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
@@ -83,6 +133,9 @@ __device__ __forceinline__ uint32_t xcd_order(uint32_t id, uint32_t total) {
   const uint32_t x = id % NXCD, q = total / NXCD, r = total % NXCD;
   return x * q + min(x, r) + id / NXCD;
 }
+
+// groups of lanes that share a joined row: up to eight, with four parts or fewer each
+inline int join_groups(int parts) { return parts <= 4 ? 1 : parts <= 8 ? 2 : parts <= 16 ? 4 : 8; }
 
 // keys of batch item b that count
 __device__ __forceinline__ int keys_of(const CrossArgs& a, int b) {

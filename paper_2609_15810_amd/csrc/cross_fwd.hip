@@ -24,12 +24,18 @@ constexpr int NW = 4;           // waves of a workgroup
 constexpr int QR = 32 * NW;     // its rows
 constexpr int KT = 64;          // keys of a tile
 
-// IDX: the keys are those of a list (a key padding mask); SPLIT: leave parts
-template <int DT, int D, bool IDX, bool SPLIT>
+// A row's exponents are relative to a reference that follows its running maximum at a distance of at most LAG (log2
+// units): it moves, and the sums are rescaled, only where the maximum has left it by more. Probabilities then reach 2^LAG,
+// which the 16-bit types and the fp32 sums hold with the same relative errors.
+constexpr float LAG = 8.f;
+
+// GATHER: addresses per key (the keys are those of a list, or their stride is too far for one buffer);
+// SPLIT: leave parts
+template <int DT, int D, bool GATHER, bool SPLIT>
 __global__ __launch_bounds__(64 * NW, 2) void cross_fwd(CrossArgs a) {
   using T = Tile<D>;
+  using C = Copier<D, KT, NW>;
   constexpr int TB = KT * T::ROW;                                // bytes of a tile
-  constexpr int COPIES = KT / T::ROWS_PER_COPY / NW;             // of a wave, per tile
   constexpr int KS = D / 16, DB = D / 32;
   __shared__ __attribute__((aligned(16))) uint8_t kt[2][TB], vt[2][TB];
 
@@ -43,28 +49,32 @@ __global__ __launch_bounds__(64 * NW, 2) void cross_fwd(CrossArgs a) {
   const int k0 = SPLIT ? split * a.chunk : 0, k1 = SPLIT ? min(n, k0 + a.chunk) : n;
   const int tiles = k1 > k0 ? (k1 - k0 + KT - 1) / KT : 0;
 
-  // the rows of a tile that this lane copies, and their tensors
   const uint16_t *kbase = a.K.p + b * a.K.sb + hk * a.K.sh, *vbase = a.V.p + b * a.V.sb + hk * a.V.sh;
   const int crow = lane / T::CH;
-  int next[COPIES];   // IDX: keys of the next tile to copy
+  const C kc(a.K.sn, wave, lane), vc(a.V.sn, wave, lane);
+  int next[C::COPIES];   // GATHER: keys of the next tile to copy
   auto fetch = [&](int t) __attribute__((always_inline)) {
-    if (IDX) {
+    if (GATHER) {
 #pragma unroll
-      for (int u = 0; u < COPIES; ++u) {
+      for (int u = 0; u < C::COPIES; ++u) {
         const int j = k0 + t * KT + (u * NW + wave) * T::ROWS_PER_COPY + crow;
-        next[u] = j < k1 ? a.idx[(size_t)b * a.N + j] : -1;
+        next[u] = j < k1 ? (a.idx ? a.idx[(size_t)b * a.N + j] : j) : -1;
       }
     }
   };
   auto copy_tile = [&](int t, int buf) __attribute__((always_inline)) {
+    if (GATHER) {
 #pragma unroll
-    for (int u = 0; u < COPIES; ++u) {
-      const int q = u * NW + wave, r = q * T::ROWS_PER_COPY + crow;
-      const int j = k0 + t * KT + r, ch = (lane % T::CH) ^ T::key(r);
-      const int64_t src = IDX ? next[u] : j;
-      const bool in = IDX ? next[u] >= 0 : j < k1;
-      copy16(in ? (const void*)(kbase + src * a.K.sn + 8 * ch) : (const void*)&zero16, kt[buf] + q * 1024);
-      copy16(in ? (const void*)(vbase + src * a.V.sn + 8 * ch) : (const void*)&zero16, vt[buf] + q * 1024);
+      for (int u = 0; u < C::COPIES; ++u) {
+        const int q = u * NW + wave, ch = (lane % T::CH) ^ T::key(q * T::ROWS_PER_COPY + crow);
+        const int64_t src = next[u];
+        copy16(src >= 0 ? (const void*)(kbase + src * a.K.sn + 8 * ch) : (const void*)&zero16, kt[buf] + q * 1024);
+        copy16(src >= 0 ? (const void*)(vbase + src * a.V.sn + 8 * ch) : (const void*)&zero16, vt[buf] + q * 1024);
+      }
+    } else {
+      const int j = k0 + t * KT;
+      kc.copy(kbase + j * a.K.sn, k1 - j, kt[buf], wave);
+      vc.copy(vbase + j * a.V.sn, k1 - j, vt[buf], wave);
     }
   };
   if (tiles > 0) {
@@ -85,7 +95,7 @@ __global__ __launch_bounds__(64 * NW, 2) void cross_fwd(CrossArgs a) {
   v16f o[DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db) o[db] = v16f{};
-  float m = -INFINITY, l = 0.f;   // l: of this lane's keys
+  float m = -INFINITY, l = 0.f;   // the reference; the sum of this lane's keys
 
   for (int t = 0; t < tiles; ++t) {
     wait_copies();
@@ -98,13 +108,14 @@ __global__ __launch_bounds__(64 * NW, 2) void cross_fwd(CrossArgs a) {
     const uint8_t *kb = kt[t & 1], *vb = vt[t & 1];
     v16f s[2];
 #pragma unroll
-    for (int g = 0; g < 2; ++g) {
-      s[g] = v16f{};
+    for (int g = 0; g < 2; ++g) s[g] = v16f{};
 #pragma unroll
-      for (int i = 0; i < KS; ++i) s[g] = mma<DT>(T::rows(kb, 32 * g, i, lane), q[i], s[g]);
-    }
+    for (int i = 0; i < KS; ++i)
+#pragma unroll
+      for (int g = 0; g < 2; ++g) s[g] = mma<DT>(T::rows(kb, 32 * g, i, lane), q[i], s[g]);
     const int valid = k1 - k0 - t * KT;
     if (valid < KT) {
+      asm volatile("");   // a branch, taken once at most, and not 32 selections in every tile
 #pragma unroll
       for (int g = 0; g < 2; ++g)
 #pragma unroll
@@ -115,8 +126,8 @@ __global__ __launch_bounds__(64 * NW, 2) void cross_fwd(CrossArgs a) {
 #pragma unroll
     for (int r = 1; r < 16; ++r) top = fmaxf(fmaxf(top, s[0][r]), s[1][r]);
     top = half_max(top) * a.c;
-    if (__builtin_amdgcn_ballot_w64(top > m)) {
-      const float up = fmaxf(m, top), alpha = __builtin_amdgcn_exp2f(m - (up == -INFINITY ? 0.f : up));
+    if (__builtin_amdgcn_ballot_w64(top > m + LAG)) {
+      const float up = top > m + LAG ? top : m, alpha = __builtin_amdgcn_exp2f(m - (up == -INFINITY ? 0.f : up));
       m = up;
       l *= alpha;
 #pragma unroll
@@ -182,26 +193,40 @@ __global__ __launch_bounds__(64 * NW, 2) void cross_fwd(CrossArgs a) {
   }
 }
 
-// The parts of a row joined: d / 4 lanes a row
+// The parts of a row joined: d / 4 lanes and `groups` (a power of two) of them share a row, group g taking the
+// parts g, g + groups, ..; the groups' sums meet in LDS. (One group walking 24 parts of the 32 rows of a token: 12 us, the
+// loads of a part waiting for the one before.)
 template <int DT, int D>
-__global__ __launch_bounds__(256) void cross_join(CrossArgs a) {
-  constexpr int L = D / 4, ROWS = 256 / L;
-  const int64_t rows = (int64_t)a.B * a.Hk * a.R, at = (int64_t)blockIdx.x * ROWS + threadIdx.x / L;
-  if (at >= rows) return;
-  const int c = threadIdx.x % L * 4;
-  float m = -INFINITY;
-  for (int s = 0; s < a.splits; ++s) m = fmaxf(m, a.part_ml[2 * (s * rows + at)]);
-  const float off = m == -INFINITY ? 0.f : m;
-  float l = 0.f;
+__global__ __launch_bounds__(256) void cross_join(CrossArgs a, int groups) {
+  constexpr int L = D / 4, ALL = 256 / L;
+  __shared__ __attribute__((aligned(16))) float so[ALL][D];
+  __shared__ float2 sml[ALL];
+  const int lane = threadIdx.x % L, slot = threadIdx.x / L, g = slot & (groups - 1), c = 4 * lane;
+  const int64_t rows = (int64_t)a.B * a.Hk * a.R, at = (int64_t)blockIdx.x * (ALL / groups) + slot / groups;
+  float m = -INFINITY, l = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int s = 0; s < a.splits; ++s) {
-    const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * (s * rows + at));
-    const float4 v = *reinterpret_cast<const float4*>(a.part_o + (s * rows + at) * D + c);
-    const float w = __builtin_amdgcn_exp2f(ml.x - off);
-    l = __builtin_fmaf(w, ml.y, l);
-    o.x = __builtin_fmaf(w, v.x, o.x), o.y = __builtin_fmaf(w, v.y, o.y);
-    o.z = __builtin_fmaf(w, v.z, o.z), o.w = __builtin_fmaf(w, v.w, o.w);
+  auto add = [&](float2 ml, float4 v) __attribute__((always_inline)) {
+    const float up = fmaxf(m, ml.x), off = up == -INFINITY ? 0.f : up;
+    const float x = __builtin_amdgcn_exp2f(m - off), w = __builtin_amdgcn_exp2f(ml.x - off);
+    m = up;
+    l = __builtin_fmaf(w, ml.y, l * x);
+    o.x = __builtin_fmaf(w, v.x, o.x * x), o.y = __builtin_fmaf(w, v.y, o.y * x);
+    o.z = __builtin_fmaf(w, v.z, o.z * x), o.w = __builtin_fmaf(w, v.w, o.w * x);
+  };
+  if (at < rows) {
+#pragma unroll 4
+    for (int s = g; s < a.splits; s += groups)
+      add(*reinterpret_cast<const float2*>(a.part_ml + 2 * (s * rows + at)),
+          *reinterpret_cast<const float4*>(a.part_o + (s * rows + at) * D + c));
   }
+  if (groups > 1) {
+    *reinterpret_cast<float4*>(&so[slot][c]) = o;
+    if (lane == 0) sml[slot] = make_float2(m, l);
+    __syncthreads();
+    if (g == 0)
+      for (int i = 1; i < groups; ++i) add(sml[slot + i], *reinterpret_cast<const float4*>(&so[slot + i][c]));
+  }
+  if (g != 0 || at >= rows) return;
   const uint32_t bh = at / a.R;
   const int b = bh / (uint32_t)a.Hk, hk = bh - b * a.Hk, n = keys_of(a, b);
   const QueryRow w = query_row(a, hk, (int)(at - (int64_t)bh * a.R));
@@ -251,15 +276,16 @@ __global__ __launch_bounds__(1024) void cross_keys(const uint8_t* mask, int64_t 
 template <int DT, int D>
 hipError_t forward(const CrossArgs& a, hipStream_t s) {
   const unsigned grid = (unsigned)((int64_t)(a.R + QR - 1) / QR * a.B * a.Hk * a.splits);
+  const bool gather = a.idx || a.K.sn >= FAR_STRIDE || a.V.sn >= FAR_STRIDE;
   if (a.splits > 1) {
-    if (a.idx) cross_fwd<DT, D, true, true><<<grid, 64 * NW, 0, s>>>(a);
+    if (gather) cross_fwd<DT, D, true, true><<<grid, 64 * NW, 0, s>>>(a);
     else cross_fwd<DT, D, false, true><<<grid, 64 * NW, 0, s>>>(a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    constexpr int ROWS = 256 / (D / 4);
-    cross_join<DT, D><<<(unsigned)(((int64_t)a.B * a.Hk * a.R + ROWS - 1) / ROWS), 256, 0, s>>>(a);
+    const int groups = join_groups(a.splits), rows = 256 / (D / 4) / groups;
+    cross_join<DT, D><<<(unsigned)(((int64_t)a.B * a.Hk * a.R + rows - 1) / rows), 256, 0, s>>>(a, groups);
   } else {
-    if (a.idx) cross_fwd<DT, D, true, false><<<grid, 64 * NW, 0, s>>>(a);
+    if (gather) cross_fwd<DT, D, true, false><<<grid, 64 * NW, 0, s>>>(a);
     else cross_fwd<DT, D, false, false><<<grid, 64 * NW, 0, s>>>(a);
   }
   return hipGetLastError();

@@ -35,13 +35,13 @@ def views(s, **kw):
 
 
 def forward(L, s, o, k_len=None, k_mask=None, stride=None, lse=FAKE, ws=FAKE, ws_bytes=1 << 40, **kw):
-    v = {n: (None if t is None else C.byref(t)) for n, t in views(s, **kw).items()}
+    v = {n: (None if t is None else bytes(t)) for n, t in views(s, **kw).items()}
     return L.vc_cross_attn_forward(C.byref(s), C.byref(o), v["Q"], v["K"], v["V"], k_len, k_mask,
                                    s.N if stride is None else stride, v["O"], lse, ws, ws_bytes, None)
 
 
 def backward(L, s, o, k_mask=None, lse=FAKE, ws=FAKE, ws_bytes=1 << 40, **kw):
-    v = {n: (None if t is None else C.byref(t)) for n, t in views(s, **kw).items()}
+    v = {n: (None if t is None else bytes(t)) for n, t in views(s, **kw).items()}
     return L.vc_cross_attn_backward(C.byref(s), C.byref(o), v["Q"], v["K"], v["V"], None, k_mask, s.N, v["O"], lse,
                                     v["dO"], v["dQ"], v["dK"], v["dV"], ws, ws_bytes, None)
 

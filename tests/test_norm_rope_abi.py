@@ -32,7 +32,7 @@ def view(s, H, data=FAKE, **kw):
 def forward(L, s, o, q=None, out=None, pos=None, cos=FAKE, k="own", weight=None):
     q = q or view(s, s.Hq)
     kv = view(s, max(s.Hk, 1)) if k == "own" else k
-    ref = lambda v: None if v is None else C.byref(v)  # noqa: E731
+    ref = lambda v: None if v is None else bytes(v)  # noqa: E731
     return L.vc_norm_rope(C.byref(s), C.byref(o), ref(q), ref(kv), weight, None, cos, FAKE, pos,
                           ref(out or view(s, s.Hq)), ref(kv), None)
 
@@ -40,7 +40,7 @@ def forward(L, s, o, q=None, out=None, pos=None, cos=FAKE, k="own", weight=None)
 def backward(L, s, o, ws=FAKE, ws_bytes=1 << 40, dw=FAKE, q="own"):
     q = view(s, s.Hq) if q == "own" else q
     v, k = view(s, s.Hq), view(s, max(s.Hk, 1))
-    r = lambda t: None if t is None else C.byref(t)  # noqa: E731
+    r = lambda t: None if t is None else bytes(t)  # noqa: E731
     return L.vc_norm_rope_backward(C.byref(s), C.byref(o), r(q), r(k), None, None, FAKE, FAKE, None, r(v), r(k), r(v),
                                    r(k), dw, None, ws, ws_bytes, None)
 
