@@ -13,7 +13,7 @@ OBJ = os.path.join(ROOT, "_build")
 LIB = os.path.join(HERE, "libvcattn.so")
 SOURCES = ["api.hip", "prep.hip", "forward.hip", "group.hip", "block_api.hip", "norm_rope.hip", "cross_fwd.hip",
            "cross_bwd.hip"]
-HEADERS = ["vc_common.hpp", "vc_internal.hpp", "cross_common.hpp"]
+HEADERS = ["vc_common.hpp", "vc_internal.hpp", "cross_common.hpp", "lanes.hpp"]
 PROBE = os.path.join(HERE, "mfma_probe")
 
 # -ffp-contract=off: every fp32 operation that decides a stored code is a single IEEE operation,

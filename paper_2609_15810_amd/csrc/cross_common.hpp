@@ -1,10 +1,14 @@
 // Device helpers shared by the cross attention's forward and backward kernels (not part of the public ABI).
 #pragma once
+#include "lanes.hpp"
 #include "vc_common.hpp"
 #include "vc_internal.hpp"
 
 namespace vc {
 namespace cross {
+
+using lanes::half_max;
+using lanes::half_sum;
 
 constexpr int NXCD = 8;   // accelerator complex dies (each with its own L2)
 
@@ -21,29 +25,6 @@ __device__ __forceinline__ v16f mma(u4 a, u4 b, v16f c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(b8, a), __builtin_bit_cast(b8, b), c, 0, 0, 0);
   else
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f8, a), __builtin_bit_cast(f8, b), c, 0, 0, 0);
-}
-
-// Empty asm that reads and rewrites x: what the compiler knows of x's value ends here
-template <typename V>
-__device__ __forceinline__ void pin(V& x) {
-  asm volatile("" : "+v"(x));
-}
-
-// sum and maximum of v over lanes l and l ^ 32 (the other half of a column's results). The swap's two results are both
-// halves' values; they are pinned, since a maximum over them has been compiled into one over a single one.
-__device__ __forceinline__ float half_sum(float v) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  uint32_t x = r[0], y = r[1];
-  pin(x);
-  pin(y);
-  return __uint_as_float(x) + __uint_as_float(y);
-}
-__device__ __forceinline__ float half_max(float v) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  uint32_t x = r[0], y = r[1];
-  pin(x);
-  pin(y);
-  return fmaxf(__uint_as_float(x), __uint_as_float(y));
 }
 
 // Tiles of rows of D 16-bit values in LDS, without padding: the 16-byte piece `ch` of row `r` stands in place

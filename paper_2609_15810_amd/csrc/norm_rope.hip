@@ -12,9 +12,11 @@
 // So a lane holds 16 channels of a row as two 16-byte pieces, d/16 lanes a row, chosen such that both channels
 // of every pair are in one lane: in the half layout pieces j and j + rot/16, which hold channels c and
 // c + rot/2; in the interleaved layout pieces j and j + d/16. The sums of a norm are exchanges among the lanes of
-// the row (or token). A wave works on 64/(16 or 8) = 8 or more rows at once: P slots of d/16 lanes each belong to
-// one token, the remaining factor is over tokens, so that a token's table row is read once per wave and
-// held for its heads. All sums are fp32, outputs are rounded once.
+// the row (or token). A wave works on 8 rows (d = 128; 16 of d = 64) at once: P slots of d/16 lanes each belong to one
+// token, the remaining factor is over tokens, so that a token's table row is read once and held for its heads. A norm
+// over more heads than two rounds of a wave's slots takes 2 or 4 waves a token, whose sums meet in LDS. All sums are
+// fp32, outputs are rounded once.
+#include "lanes.hpp"
 #include "vc_common.hpp"
 #include "vc_internal.hpp"
 
@@ -48,17 +50,31 @@ __device__ __forceinline__ u4 pack8(const float* x) {
   return out;
 }
 
+// The channels of a lane: two pieces of 8, starting at c0 and c1; which of its pairs are turned
+struct Lane {
+  int c0, c1;       // first channels of its pieces
+  bool turn0, turn1;
+};
+
+// A row's two pieces. Results of large calls are stored past the caches (past_caches)
+__device__ __forceinline__ void store_row(uint16_t* row, const Lane& l, u4 lo, u4 hi, int past) {
+  if (past) {
+    asm volatile("" ::: "memory");   // without these, both branches become one of plain stores
+    __builtin_nontemporal_store(lo, reinterpret_cast<u4*>(row + l.c0));
+    __builtin_nontemporal_store(hi, reinterpret_cast<u4*>(row + l.c1));
+    asm volatile("" ::: "memory");
+  } else {
+    *reinterpret_cast<u4*>(row + l.c0) = lo;
+    *reinterpret_cast<u4*>(row + l.c1) = hi;
+  }
+}
+
 __device__ __forceinline__ void load8f(const float* p, float* x) {
   const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
   x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w;
   x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
 }
 
-// The channels of a lane: two pieces of 8, starting at c0 and c1; which of its pairs are turned
-struct Lane {
-  int c0, c1;       // first channels of its pieces
-  bool turn0, turn1;
-};
 template <int D, int LAYOUT>
 __device__ __forceinline__ Lane lane_channels(int j, int rot) {
   constexpr int G = D / 16;
@@ -111,14 +127,19 @@ __device__ __forceinline__ void load_angles(const NormRopeArgs& a, const Lane& l
     for (int q = 0; q < 2; ++q) {
       const int p = q ? p1 : p0;
       const int first = rope_axis(p), last = rope_axis(p + 3);
-      const int ra = pick(first) + p, rb = pick(last) + p;
+      const int ra = pick(first) + p;
       const float4 ca = *reinterpret_cast<const float4*>(a.cos_t + ra), sa = *reinterpret_cast<const float4*>(a.sin_t + ra);
-      const float4 cb = *reinterpret_cast<const float4*>(a.cos_t + rb), sb = *reinterpret_cast<const float4*>(a.sin_t + rb);
-      const bool s1 = rope_axis(p + 1) == first, s2 = rope_axis(p + 2) == first;
-      cs[4 * q] = ca.x, sn[4 * q] = sa.x;
-      cs[4 * q + 1] = s1 ? ca.y : cb.y, sn[4 * q + 1] = s1 ? sa.y : sb.y;
-      cs[4 * q + 2] = s2 ? ca.z : cb.z, sn[4 * q + 2] = s2 ? sa.z : sb.z;
-      cs[4 * q + 3] = cb.w, sn[4 * q + 3] = sb.w;
+      float *c = cs + 4 * q, *s = sn + 4 * q;
+      c[0] = ca.x, c[1] = ca.y, c[2] = ca.z, c[3] = ca.w;
+      s[0] = sa.x, s[1] = sa.y, s[2] = sa.z, s[3] = sa.w;
+      if (first != last) {   // in two of a row's sixteen groups: a load of few lanes
+        const int rb = pick(last) + p;
+        const float4 cb = *reinterpret_cast<const float4*>(a.cos_t + rb), sb = *reinterpret_cast<const float4*>(a.sin_t + rb);
+        const bool s1 = rope_axis(p + 1) == first, s2 = rope_axis(p + 2) == first;
+        c[1] = s1 ? c[1] : cb.y, s[1] = s1 ? s[1] : sb.y;
+        c[2] = s2 ? c[2] : cb.z, s[2] = s2 ? s[2] : sb.z;
+        c[3] = cb.w, s[3] = sb.w;
+      }
     }
   }
 #pragma unroll
@@ -138,91 +159,145 @@ __device__ __forceinline__ void turn(float* x, const float* cs, const float* sn)
   }
 }
 
-// sum over the `n` lanes (a power of two) that a lane shares a span with
+// sum over the n lanes (4, 8, .., 64) that a lane shares a span with: exchanges in quads, mirrored in 8 and 16 lanes
+// (where all lanes of a half have the same sum by then), and of the wave's quarters and halves
+template <int CTRL>
+__device__ __forceinline__ float dpp_add(float v) {
+  return v + __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xf, 0xf, true));
+}
 __device__ __forceinline__ float lanes_sum(float v, int n) {
-  for (int o = 1; o < n; o <<= 1) v += __shfl_xor(v, o, 64);
+  v = dpp_add<0xb1>(v);                // quad_perm 1 0 3 2
+  v = dpp_add<0x4e>(v);                // quad_perm 2 3 0 1
+  if (n > 4) v = dpp_add<0x141>(v);    // row_half_mirror
+  if (n > 8) v = dpp_add<0x140>(v);    // row_mirror
+  if (n > 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    uint32_t x = r[0], y = r[1];
+    lanes::pin(x);
+    lanes::pin(y);
+    v = __uint_as_float(x) + __uint_as_float(y);
+  }
+  if (n > 32) v = lanes::half_sum(v);
   return v;
 }
 
-// Where a wave's slots stand: slot = lane / (d/16); token slot / P of the wave's 64/(d/16)/P, head slot % P
+// Where a wave's slots stand. A workgroup's waves form WAVES / W teams of W waves; a team works on one group of
+// tokens: one token where P, the slots of a token, is all of the team's, else 64 / (d/16) / P of them.
 struct Place {
-  int j, b, n, head;   // lane in its row, batch item, token, first head
-  bool live;
+  int b, n, head;   // batch item, token, first head
+  int live;         // 0: behind the last token
 };
 template <int D>
-__device__ __forceinline__ Place place(const NormRopeArgs& a, int P, int64_t group, int head0) {
+__device__ __forceinline__ Place place(const NormRopeArgs& a, const NormRopeTensor& x, int wave, uint32_t group, int head0) {
   constexpr int G = D / 16, SLOTS = 64 / G;
-  const int lane = threadIdx.x & 63, slot = lane / G;
+  const int slot = (wave & (x.W - 1)) * SLOTS + (threadIdx.x & 63) / G;
   Place p;
-  p.j = lane % G;
-  const int tokens = SLOTS / P;
-  const int64_t t = group * tokens + slot / P;
-  p.head = head0 + (slot & (P - 1));
-  p.live = t < a.tokens;
-  const int64_t tt = p.live ? t : a.tokens - 1;
-  p.b = (int)(tt / a.N);
-  p.n = (int)(tt - (int64_t)p.b * a.N);
+  const uint32_t t = group * (SLOTS * x.W / x.P) + slot / x.P;   // below 2^31 + 32
+  p.head = head0 + (slot & (x.P - 1));
+  p.live = t < (uint32_t)a.tokens;
+  const uint32_t tt = p.live ? t : (uint32_t)a.tokens - 1;
+  p.b = a.N == (int)a.tokens ? 0 : tt / (uint32_t)a.N;
+  p.n = tt - p.b * a.N;
   return p;
 }
 
-// One wave: the heads head0, head0 + P, .. of its tokens, at most `heads` iterations, NB of them in flight at once.
-// A norm over the token needs all heads in one batch (heads <= NB).
+// Sums over a token of the waves of its team (each lane of a wave has its wave's); `red` alternates between two rounds, so
+// one barrier a round is enough
+template <int K>
+__device__ __forceinline__ void team_sum(float (&v)[K], float (&red)[WAVES][K], int wave, int W) {
+  if (W == 1) return;
+  if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) red[wave][k] = v[k];
+  }
+  __syncthreads();
+  const int first = wave & ~(W - 1);
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    v[k] = red[first][k];
+    for (int w = 1; w < W; ++w) v[k] += red[first + w][k];
+  }
+}
+
+// The teams of a tensor walk over its units: a group of tokens with the heads h, h + P, .. of one batch of NB heads a
+// slot (a norm over the token has all heads in one batch). The rows of the next unit are loaded while the present one
+// is worked on; the weights stay in registers.
 template <int DT, int D, int NORM, int LAYOUT, int NB>
-__global__ __launch_bounds__(64 * WAVES) void norm_rope_fwd(NormRopeArgs a) {
+__global__ __launch_bounds__(64 * WAVES, 3) void norm_rope_fwd(NormRopeArgs a) {
+  __shared__ float red[2][WAVES][1];
   const NormRopeTensor& x = a.t[blockIdx.y];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t w = (int64_t)blockIdx.x * WAVES + wave;
-  const int64_t group = w / x.parts;   // tokens of the wave; part of the heads
-  const int part = (int)(w - group * x.parts);
-  constexpr int G = D / 16, SLOTS = 64 / G;
-  const int P = x.P;
-  if (group * (SLOTS / P) >= a.tokens) return;
-  const Place p = place<D>(a, P, group, part * x.iters * P);
-  const int end = min(x.H, (part + 1) * x.iters * P);
-  const Lane l = lane_channels<D, LAYOUT>(p.j, a.rot);
-  const uint16_t* in = x.in + p.b * x.in_sb + p.n * x.in_sn;
-  uint16_t* out = x.out + p.b * x.out_sb + p.n * x.out_sn;
-  float cs[8], sn[8], wt[16];
-  u4 raw[NB][2];
-  auto load = [&](int h0) __attribute__((always_inline)) {
+  constexpr int G = D / 16;
+  constexpr int NW = NORM == VC_NORM_TOKEN ? NB : 1;   // weights that a lane meets: its channels of so many heads
+  const int P = x.P, per = NB * P, teams = WAVES / x.W;
+  const uint32_t batches = (x.H + per - 1) / per;
+  const uint64_t units = (uint64_t)x.groups * batches;
+  uint64_t first = (uint64_t)blockIdx.x * teams;   // of the workgroup: the same for its waves, which share barriers
+  if (first >= units) return;
+  const Lane l = lane_channels<D, LAYOUT>(threadIdx.x & (G - 1), a.rot);
+  auto at = [&](uint64_t u) __attribute__((always_inline)) {
+    u += wave / x.W;
+    if (batches == 1) return place<D>(a, x, wave, (uint32_t)u, 0);
+    const uint32_t group = u / batches;
+    return place<D>(a, x, wave, group, (int)(u - (uint64_t)group * batches) * per);
+  };
+  auto load = [&](const Place& p, u4 (&raw)[NB][2]) __attribute__((always_inline)) {
+    const uint16_t* in = x.in + p.b * x.in_sb + p.n * x.in_sn;
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
-      const int h = h0 + i * P;
-      if (p.live && h < end) {
+      const int h = p.head + i * P;
+      raw[i][0] = raw[i][1] = u4{0, 0, 0, 0};
+      if (p.live && h < x.H) {
         const uint16_t* row = in + h * x.in_sh;
         raw[i][0] = *reinterpret_cast<const u4*>(row + l.c0);
         raw[i][1] = *reinterpret_cast<const u4*>(row + l.c1);
-      } else {
-        raw[i][0] = raw[i][1] = u4{0, 0, 0, 0};
       }
     }
   };
-  load(p.head);
-  load_angles<LAYOUT>(a, l, p.n, p.b, a.sign, cs, sn);
-  if (NORM == VC_NORM_HEAD && x.weight) {
-    load8f(x.weight + l.c0, wt);
-    load8f(x.weight + l.c1, wt + 8);
-  } else {
+  Place p = at(first);
+  u4 raw[NB][2];
+  load(p, raw);
+  float wt[NW][16];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) wt[e] = 1.f;
+  for (int i = 0; i < NW; ++i) {
+    const int h = NORM == VC_NORM_TOKEN ? p.head + i * P : 0;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) wt[i][e] = 1.f;
+    if (NORM != VC_NORM_NONE && x.weight && h < x.H) {
+      load8f(x.weight + h * D + l.c0, wt[i]);
+      load8f(x.weight + h * D + l.c1, wt[i] + 8);
+    }
   }
-  for (int h0 = p.head; ; ) {
-    float ss = 0.f;
+  for (int round = 0;; round ^= 1) {
+    float cs[8], sn[8];
+    load_angles<LAYOUT>(a, l, p.n, p.b, a.sign, cs, sn);
+    first += (uint64_t)gridDim.x * teams;
+    const bool more = first < units;
+    Place np = p;
+    u4 next[NB][2];
+    if (more) {
+      np = at(first);
+      load(np, next);
+    }
+    float r = 1.f;
     if (NORM == VC_NORM_TOKEN) {
+      float ss[1] = {0.f};
 #pragma unroll
       for (int i = 0; i < NB; ++i) {
         float v[16];
         unpack8<DT>(raw[i][0], v);
         unpack8<DT>(raw[i][1], v + 8);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) ss = __builtin_fmaf(v[e], v[e], ss);
+        for (int e = 0; e < 16; ++e) ss[0] = __builtin_fmaf(v[e], v[e], ss[0]);
       }
-      ss = lanes_sum(ss, G * P);
+      ss[0] = lanes_sum(ss[0], min(G * P, 64));
+      team_sum(ss, red[round], wave, x.W);
+      r = __builtin_amdgcn_rsqf(__builtin_fmaf(ss[0], x.inv_span, a.eps));
     }
-    float r = NORM == VC_NORM_TOKEN ? __builtin_amdgcn_rsqf(__builtin_fmaf(ss, x.inv_span, a.eps)) : 1.f;
+    uint16_t* out = x.out + p.b * x.out_sb + p.n * x.out_sn;
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
-      const int h = h0 + i * P;
+      const int h = p.head + i * P;
       float v[16];
       unpack8<DT>(raw[i][0], v);
       unpack8<DT>(raw[i][1], v + 8);
@@ -232,81 +307,90 @@ __global__ __launch_bounds__(64 * WAVES) void norm_rope_fwd(NormRopeArgs a) {
         for (int e = 0; e < 16; ++e) s = __builtin_fmaf(v[e], v[e], s);
         r = __builtin_amdgcn_rsqf(__builtin_fmaf(lanes_sum(s, G), x.inv_span, a.eps));
       }
-      const bool on = p.live && h < end;
-      if (NORM == VC_NORM_TOKEN && x.weight && on) {
-        load8f(x.weight + h * D + l.c0, wt);
-        load8f(x.weight + h * D + l.c1, wt + 8);
-      }
       if (NORM != VC_NORM_NONE) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) v[e] = v[e] * r * wt[e];
+        for (int e = 0; e < 16; ++e) v[e] = v[e] * r * wt[NORM == VC_NORM_TOKEN ? i : 0][e];
       }
       turn<LAYOUT>(v, cs, sn);
-      if (on) {
-        uint16_t* row = out + h * x.out_sh;
-        *reinterpret_cast<u4*>(row + l.c0) = pack8<DT>(v);
-        *reinterpret_cast<u4*>(row + l.c1) = pack8<DT>(v + 8);
+      if (p.live && h < x.H) {
+        store_row(out + h * x.out_sh, l, pack8<DT>(v), pack8<DT>(v + 8), a.past);
       }
     }
-    h0 += NB * P;
-    if (NORM == VC_NORM_TOKEN || h0 - p.head + part * x.iters * P >= end) break;   // the same for all lanes
-    load(h0);
+    if (!more) break;
+    p = np;
+#pragma unroll
+    for (int i = 0; i < NB; ++i) raw[i][0] = next[i][0], raw[i][1] = next[i][1];
   }
 }
 
-// Gradients. Waves walk over the tokens (groups wave, wave + waves of the grid, ..), so that the sums of the
-// weights' gradients stay in registers; a workgroup's waves add theirs in LDS one after the other, in a fixed order,
-// and write one row of partial sums, which norm_rope_join adds up in a fixed order.
+// Gradients. The teams walk over the units as in the forward kernel (all batches of a group of tokens by the same team), so
+// that the sums of the weights' gradients stay in registers; a workgroup's waves add theirs in LDS one after the other, in a
+// fixed order, and write one row of partial sums, which norm_rope_join adds up in a fixed order.
 template <int DT, int D, int NORM, int LAYOUT, int NB>
-__global__ __launch_bounds__(64 * WAVES) void norm_rope_bwd(NormRopeArgs a) {
+__global__ __launch_bounds__(64 * WAVES, 2) void norm_rope_bwd(NormRopeArgs a) {
   extern __shared__ float acc[];
+  __shared__ float red[2][WAVES][2];
   const NormRopeTensor& x = a.t[blockIdx.y];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  constexpr int G = D / 16, SLOTS = 64 / G;
-  constexpr int ND = NORM == VC_NORM_TOKEN ? NB : 1;   // weights that a lane meets: its 16 channels of so many heads
-  const int P = x.P, tokens = SLOTS / P;
-  const int64_t groups = (a.tokens + tokens - 1) / tokens;
-  float dw[ND][16], wt[16];
+  constexpr int G = D / 16;
+  constexpr int NW = NORM == VC_NORM_TOKEN ? NB : 1;
+  const int P = x.P, teams = WAVES / x.W, lane = threadIdx.x & 63;
+  const Lane l = lane_channels<D, LAYOUT>(lane % G, a.rot);
+  const int head0 = place<D>(a, x, wave, 0, 0).head;   // a slot's heads are the same in all groups
+  float dw[NW][16], wt[NW][16];
 #pragma unroll
-  for (int i = 0; i < ND; ++i)
+  for (int i = 0; i < NW; ++i) {
+    const int h = NORM == VC_NORM_TOKEN ? head0 + i * P : 0;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) dw[i][e] = 0.f;
-  const int lane = threadIdx.x & 63, j = lane % G;
-  const Lane l = lane_channels<D, LAYOUT>(j, a.rot);
-#pragma unroll
-  for (int e = 0; e < 16; ++e) wt[e] = 1.f;
-  if (NORM == VC_NORM_HEAD && x.weight) {
-    load8f(x.weight + l.c0, wt);
-    load8f(x.weight + l.c1, wt + 8);
+    for (int e = 0; e < 16; ++e) dw[i][e] = 0.f, wt[i][e] = 1.f;
+    if (x.weight && h < x.H) {
+      load8f(x.weight + h * D + l.c0, wt[i]);
+      load8f(x.weight + h * D + l.c1, wt[i] + 8);
+    }
   }
-  for (int64_t group = (int64_t)blockIdx.x * WAVES + wave; group < groups; group += (int64_t)gridDim.x * WAVES) {
-    const Place p = place<D>(a, P, group, 0);
-    const uint16_t* in = x.in + p.b * x.in_sb + p.n * x.in_sn;
-    const uint16_t* gin = x.grad + p.b * x.grad_sb + p.n * x.grad_sn;
-    uint16_t* out = x.out + p.b * x.out_sb + p.n * x.out_sn;
-    float cs[8], sn[8];
-    bool angles = false;
-    for (int h0 = p.head;;) {
-      u4 raw[NB][2], gr[NB][2];
+  const int per = NB * P;
+  struct Unit {
+    Place p;
+    int h0;
+    uint64_t first;
+  };
+  auto load = [&](const Unit& u, u4 (&raw)[NB][2], u4 (&gr)[NB][2]) __attribute__((always_inline)) {
+    const uint16_t* in = x.in + u.p.b * x.in_sb + u.p.n * x.in_sn;
+    const uint16_t* gin = x.grad + u.p.b * x.grad_sb + u.p.n * x.grad_sn;
 #pragma unroll
-      for (int i = 0; i < NB; ++i) {
-        const int h = h0 + i * P;
-        raw[i][0] = raw[i][1] = gr[i][0] = gr[i][1] = u4{0, 0, 0, 0};
-        if (p.live && h < x.H) {
-          raw[i][0] = *reinterpret_cast<const u4*>(in + h * x.in_sh + l.c0);
-          raw[i][1] = *reinterpret_cast<const u4*>(in + h * x.in_sh + l.c1);
-          gr[i][0] = *reinterpret_cast<const u4*>(gin + h * x.grad_sh + l.c0);
-          gr[i][1] = *reinterpret_cast<const u4*>(gin + h * x.grad_sh + l.c1);
-        }
+    for (int i = 0; i < NB; ++i) {
+      const int h = u.h0 + i * P;
+      raw[i][0] = raw[i][1] = gr[i][0] = gr[i][1] = u4{0, 0, 0, 0};
+      if (u.p.live && h < x.H) {
+        raw[i][0] = *reinterpret_cast<const u4*>(in + h * x.in_sh + l.c0);
+        raw[i][1] = *reinterpret_cast<const u4*>(in + h * x.in_sh + l.c1);
+        gr[i][0] = *reinterpret_cast<const u4*>(gin + h * x.grad_sh + l.c0);
+        gr[i][1] = *reinterpret_cast<const u4*>(gin + h * x.grad_sh + l.c1);
       }
-      if (!angles) load_angles<LAYOUT>(a, l, p.n, p.b, -1.f, cs, sn);
-      angles = true;
-      auto weights = [&](int h) __attribute__((always_inline)) {
-        if (NORM == VC_NORM_TOKEN && x.weight && h < x.H) {
-          load8f(x.weight + h * D + l.c0, wt);
-          load8f(x.weight + h * D + l.c1, wt + 8);
-        }
-      };
+    }
+  };
+  Unit u;
+  u.first = (uint64_t)blockIdx.x * teams;
+  u.h0 = head0;
+  u4 raw[NB][2], gr[NB][2];
+  if (u.first < x.groups) {
+    u.p = place<D>(a, x, wave, (uint32_t)(u.first + wave / x.W), 0);
+    load(u, raw, gr);
+    float cs[8], sn[8];
+    for (int round = 0;; round ^= 1) {
+      if (u.h0 == head0) load_angles<LAYOUT>(a, l, u.p.n, u.p.b, -1.f, cs, sn);
+      // the next batch of the heads, or the next tokens
+      Unit v = u;
+      v.h0 += per;
+      if (v.h0 - head0 >= x.H) {
+        v.h0 = head0;
+        v.first += (uint64_t)gridDim.x * teams;
+        v.p = place<D>(a, x, wave, (uint32_t)(v.first + wave / x.W), 0);
+      }
+      const bool more = v.first < x.groups;
+      u4 raw_next[NB][2], gr_next[NB][2];
+      if (more) load(v, raw_next, gr_next);
+      uint16_t* out = x.out + u.p.b * x.out_sb + u.p.n * x.out_sn;
       auto values = [&](int i, float* v, float* g) __attribute__((always_inline)) {
         unpack8<DT>(raw[i][0], v);
         unpack8<DT>(raw[i][1], v + 8);
@@ -314,63 +398,60 @@ __global__ __launch_bounds__(64 * WAVES) void norm_rope_bwd(NormRopeArgs a) {
         unpack8<DT>(gr[i][1], g + 8);
         turn<LAYOUT>(g, cs, sn);
       };
-      float r = 0.f, k = 0.f;   // r, and r^3 mean(g w x)
-      auto sums = [&](float ss, float dot, int lanes) __attribute__((always_inline)) {
-        ss = lanes_sum(ss, lanes);
-        dot = lanes_sum(dot, lanes);
-        r = __builtin_amdgcn_rsqf(__builtin_fmaf(ss, x.inv_span, a.eps));
-        k = r * r * r * (dot * x.inv_span);
+      float t[2] = {0.f, 0.f};   // sums of x^2 and of g w x
+      auto add = [&](int i, const float* v, const float* g) __attribute__((always_inline)) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          t[0] = __builtin_fmaf(v[e], v[e], t[0]);
+          t[1] = __builtin_fmaf(v[e] * wt[NORM == VC_NORM_TOKEN ? i : 0][e], g[e], t[1]);
+        }
       };
       if (NORM == VC_NORM_TOKEN) {
-        float ss = 0.f, dot = 0.f;
 #pragma unroll
         for (int i = 0; i < NB; ++i) {
           float v[16], g[16];
           values(i, v, g);
-          weights(h0 + i * P);
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            ss = __builtin_fmaf(v[e], v[e], ss);
-            dot = __builtin_fmaf(v[e] * wt[e], g[e], dot);
-          }
+          add(i, v, g);
         }
-        sums(ss, dot, G * P);
+        t[0] = lanes_sum(t[0], min(G * P, 64));
+        t[1] = lanes_sum(t[1], min(G * P, 64));
+        team_sum(t, red[round], wave, x.W);
       }
 #pragma unroll
       for (int i = 0; i < NB; ++i) {
-        const int h = h0 + i * P;
+        const int h = u.h0 + i * P, iw = NORM == VC_NORM_TOKEN ? i : 0;
         float v[16], g[16];
         values(i, v, g);
-        weights(h);
         if (NORM == VC_NORM_HEAD) {
-          float ss = 0.f, dot = 0.f;
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            ss = __builtin_fmaf(v[e], v[e], ss);
-            dot = __builtin_fmaf(v[e] * wt[e], g[e], dot);
-          }
-          sums(ss, dot, G);
+          t[0] = t[1] = 0.f;
+          add(i, v, g);
+          t[0] = lanes_sum(t[0], G);
+          t[1] = lanes_sum(t[1], G);
         }
+        const float r = __builtin_amdgcn_rsqf(__builtin_fmaf(t[0], x.inv_span, a.eps));
+        const float k = r * r * r * (t[1] * x.inv_span);   // r^3 mean(g w x)
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          const int id = NORM == VC_NORM_TOKEN ? i : 0;
-          dw[id][e] = __builtin_fmaf(g[e] * r, v[e], dw[id][e]);
-          g[e] = __builtin_fmaf(-k, v[e], g[e] * wt[e] * r);
+          dw[iw][e] = __builtin_fmaf(g[e] * r, v[e], dw[iw][e]);
+          g[e] = __builtin_fmaf(-k, v[e], g[e] * wt[iw][e] * r);
         }
-        if (p.live && h < x.H) {
-          *reinterpret_cast<u4*>(out + h * x.out_sh + l.c0) = pack8<DT>(g);
-          *reinterpret_cast<u4*>(out + h * x.out_sh + l.c1) = pack8<DT>(g + 8);
+        if (u.p.live && h < x.H) {
+          store_row(out + h * x.out_sh, l, pack8<DT>(g), pack8<DT>(g + 8), a.past);
         }
       }
-      h0 += NB * P;
-      if (NORM == VC_NORM_TOKEN || h0 - p.head >= x.H) break;
+      if (!more) break;
+      u = v;
+#pragma unroll
+      for (int i = 0; i < NB; ++i)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) raw[i][e] = raw_next[i][e], gr[i][e] = gr_next[i][e];
     }
   }
   if (!x.dw_part) return;
   // slots that share their channels: all of the wave (a head's norm), or those of its other tokens
-  const int share = NORM == VC_NORM_HEAD ? G : G * P;
+  const int share = NORM == VC_NORM_HEAD ? G : min(G * P, 64);
 #pragma unroll
-  for (int i = 0; i < ND; ++i)
+  for (int i = 0; i < NW; ++i)
 #pragma unroll
     for (int e = 0; e < 16; ++e)
       for (int o = share; o < 64; o <<= 1) dw[i][e] += __shfl_xor(dw[i][e], o, 64);
@@ -378,13 +459,13 @@ __global__ __launch_bounds__(64 * WAVES) void norm_rope_bwd(NormRopeArgs a) {
   for (int w = 0; w < WAVES; ++w) {
     if (w == wave && lane < share) {
 #pragma unroll
-      for (int i = 0; i < ND; ++i) {
-        const int h = NORM == VC_NORM_HEAD ? 0 : lane / G + i * P;
+      for (int i = 0; i < NW; ++i) {
+        const int h = NORM == VC_NORM_HEAD ? 0 : head0 + i * P;
         if (NORM == VC_NORM_HEAD || h < x.H) {
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
             const int c = h * D + (e < 8 ? l.c0 + e : l.c1 + e - 8);
-            acc[c] = w == 0 ? dw[i][e] : acc[c] + dw[i][e];
+            acc[c] = w < x.W ? dw[i][e] : acc[c] + dw[i][e];   // the first team's waves have all channels
           }
         }
       }
@@ -394,18 +475,21 @@ __global__ __launch_bounds__(64 * WAVES) void norm_rope_bwd(NormRopeArgs a) {
   for (int c = threadIdx.x; c < C; c += 64 * WAVES) x.dw_part[(size_t)blockIdx.x * C + c] = acc[c];
 }
 
-// dw[c] = sum of the partial rows: 16 channels a workgroup, 16 threads a channel walk the rows, a tree adds them
-__global__ __launch_bounds__(256) void norm_rope_join(NormRopeArgs a, int parts) {
-  __shared__ float s[16][17];
+// dw[c] = sum of the partial rows: 8 channels a workgroup, 128 threads a channel walk the rows, a tree adds them
+// (with 16 threads a channel, 64 loads one behind the other: 25 us for 128 channels of 1024 rows)
+__global__ __launch_bounds__(1024) void norm_rope_join(NormRopeArgs a, int parts) {
+  __shared__ float s[128][9];
   const NormRopeTensor& x = a.t[blockIdx.y];
   const int C = x.weights;
-  const int cc = threadIdx.x & 15, row = threadIdx.x >> 4, c = blockIdx.x * 16 + cc;
+  const int cc = threadIdx.x & 7, row = threadIdx.x >> 3, c = blockIdx.x * 8 + cc;
   float v = 0.f;
-  if (x.dw_part && c < C)
-    for (int p = row; p < parts; p += 16) v += x.dw_part[(size_t)p * C + c];
+  if (x.dw_part && c < C) {
+#pragma unroll 4
+    for (int p = row; p < parts; p += 128) v += x.dw_part[(size_t)p * C + c];
+  }
   s[row][cc] = v;
   __syncthreads();
-  for (int o = 8; o > 0; o >>= 1) {
+  for (int o = 64; o > 0; o >>= 1) {
     if (row < o) s[row][cc] += s[row + o][cc];
     __syncthreads();
   }
@@ -422,16 +506,10 @@ hipError_t launch(const NormRopeArgs& a, int grid, size_t lds, hipStream_t s) {
 
 template <int DT, int D, int NORM, int LAYOUT, bool BWD>
 hipError_t launch_nb(const NormRopeArgs& a, int nb, int grid, size_t lds, hipStream_t s) {
-  if constexpr (NORM == VC_NORM_TOKEN) {
-    if (nb <= 1) return launch<DT, D, NORM, LAYOUT, 1, BWD>(a, grid, lds, s);
-    if (nb <= 2) return launch<DT, D, NORM, LAYOUT, 2, BWD>(a, grid, lds, s);
-    if (nb <= 4) return launch<DT, D, NORM, LAYOUT, 4, BWD>(a, grid, lds, s);
-    if (nb <= 5) return launch<DT, D, NORM, LAYOUT, 5, BWD>(a, grid, lds, s);
-    return launch<DT, D, NORM, LAYOUT, 8, BWD>(a, grid, lds, s);
-  } else {
-    if (nb <= 1) return launch<DT, D, NORM, LAYOUT, 1, BWD>(a, grid, lds, s);
-    return launch<DT, D, NORM, LAYOUT, 2, BWD>(a, grid, lds, s);
-  }
+  if (nb <= 1) return launch<DT, D, NORM, LAYOUT, 1, BWD>(a, grid, lds, s);
+  if constexpr (NORM != VC_NORM_TOKEN && !BWD)
+    if (nb > 2) return launch<DT, D, NORM, LAYOUT, 4, BWD>(a, grid, lds, s);
+  return launch<DT, D, NORM, LAYOUT, 2, BWD>(a, grid, lds, s);
 }
 
 template <int DT, int D, int NORM, bool BWD>
@@ -459,12 +537,28 @@ hipError_t dispatch(const NormRopeArgs& a, int nb, int grid, size_t lds, hipStre
                             : launch_norm<VC_FP16, 64, BWD>(a, nb, grid, lds, s);
 }
 
-// slots of a wave that a token's heads take: as many as there are heads, up to the whole wave
-int slots_of(int H, int d) {
-  const int most = 64 / (d / 16);
-  int P = 1;
-  while (P < most && P < H) P *= 2;
-  return P;
+// Waves of a team, slots of a token and groups of tokens of a tensor; returns the rounds of the slots over its heads
+int set_teams(const NormRopeArgs& a, NormRopeTensor& t) {
+  const int slots = 64 / (a.d / 16);   // of a wave
+  t.W = 1;
+  if (a.norm == VC_NORM_TOKEN)
+    while (t.W < WAVES && t.H > 2 * slots * t.W) t.W *= 2;   // two rounds at most (8192 channels)
+  t.P = t.W * slots;
+  if (t.W == 1)
+    while (t.P / 2 >= t.H) t.P /= 2;
+  const int tokens = slots * t.W / t.P;
+  t.groups = (uint32_t)((a.tokens + tokens - 1) / tokens);
+  return (t.H + t.P - 1) / t.P;
+}
+
+// Calls whose tensors do not stay in the 256 MB memory-side cache anyway store their results past the caches. Measured (us,
+// with / without, inputs from memory): 12 heads of 32760 tokens (200 MB in, 200 MB out) 82 / 87 the rotation alone, 86 / 91
+// norms per head, 81 / 85 norms per token, gradients 132 / 139 and 142 / 148. Smaller results stay for the step that reads
+// them next.
+int past_caches(const NormRopeArgs& a, int tensors) {
+  int64_t values = 0;
+  for (int i = 0; i < a.ntensors; ++i) values += a.tokens * a.t[i].H * a.d;
+  return values * 2 * tensors > (256LL << 20);
 }
 
 }  // namespace
@@ -472,43 +566,45 @@ int slots_of(int H, int d) {
 int norm_rope_parts(int64_t tokens) {
   // workgroups of the backward kernel, each of which leaves a row of partial weight sums
   const int64_t w = (tokens + 4 * WAVES - 1) / (4 * WAVES);
-  return (int)(w < 1 ? 1 : (w > 1024 ? 1024 : w));
+  return (int)(w < 1 ? 1 : (w > 512 ? 512 : w));
 }
 
 hipError_t launch_norm_rope(NormRopeArgs a, hipStream_t s) {
-  int64_t grid = 1;
-  int nb = 1;
+  a.past = past_caches(a, 2);
+  int64_t rounds = 1, units = 0;
   for (int i = 0; i < a.ntensors; ++i) {
-    NormRopeTensor& t = a.t[i];
-    t.P = slots_of(t.H, a.d);
-    const int tokens = 64 / (a.d / 16) / t.P, iters = (t.H + t.P - 1) / t.P;
-    const int64_t groups = (a.tokens + tokens - 1) / tokens;
-    // few tokens: the heads of a token go to several waves
-    t.parts = a.norm != VC_NORM_TOKEN && groups * iters <= 4096 ? iters : 1;
-    t.iters = (iters + t.parts - 1) / t.parts;
-    nb = t.iters > nb ? t.iters : nb;
-    const int64_t g = (groups * t.parts + WAVES - 1) / WAVES;
-    grid = g > grid ? g : grid;
+    const int64_t r = set_teams(a, a.t[i]);
+    rounds = r > rounds ? r : rounds;
+    units += a.t[i].groups * r;
   }
-  return dispatch<false>(a, nb, (int)grid, 0, s);
+  // heads of a slot that a wave has in flight: more of them for large calls; one, so that the heads of a token go to
+  // several waves, where there are few tokens
+  const int nb = a.norm == VC_NORM_TOKEN ? (int)rounds : units <= 4096 ? 1 : rounds <= 2 ? (int)rounds : 4;
+  int64_t grid = 1;
+  for (int i = 0; i < a.ntensors; ++i) {
+    const NormRopeTensor& t = a.t[i];
+    const int64_t u = (int64_t)t.groups * ((t.H + nb * t.P - 1) / (nb * t.P)), teams = WAVES / t.W;
+    grid = (u + teams - 1) / teams > grid ? (u + teams - 1) / teams : grid;
+  }
+  const int64_t most = 2048 / a.ntensors;
+  return dispatch<false>(a, nb, (int)(grid < most ? grid : most), 0, s);
 }
 
 hipError_t launch_norm_rope_backward(NormRopeArgs a, hipStream_t s) {
+  a.past = past_caches(a, 3);
   int nb = 1, C = 0;
   bool weights = false;
   for (int i = 0; i < a.ntensors; ++i) {
     NormRopeTensor& t = a.t[i];
-    t.P = slots_of(t.H, a.d);
-    t.parts = 1;
-    t.iters = (t.H + t.P - 1) / t.P;
-    nb = t.iters > nb ? t.iters : nb;
+    const int r = set_teams(a, t);
+    nb = r > nb ? r : nb;
     C = t.weights > C ? t.weights : C;
     weights = weights || t.dw_part;
   }
   const int parts = norm_rope_parts(a.tokens);
   hipError_t e = dispatch<true>(a, nb, parts, (size_t)C * 4, s);
   if (e != hipSuccess || !weights) return e;
-  norm_rope_join<<<dim3((unsigned)((C + 15) / 16), (unsigned)a.ntensors), 256, 0, s>>>(a, parts);
+  norm_rope_join<<<dim3((unsigned)((C + 7) / 8), (unsigned)a.ntensors), 1024, 0, s>>>(a, parts);
   return hipGetLastError();
 }
 

@@ -85,7 +85,8 @@ struct NormRopeTensor {
   float* dw_part;        // [workgroups][weights] partial sums, or null (no weight gradient)
   float inv_span;        // 1 / channels under one norm
   int H, weights;
-  int P, parts, iters;   // head slots of a wave; waves that share a token's heads; iterations of a wave over them
+  int W, P;              // waves that share a token; slots of theirs that work on its heads
+  uint32_t groups;       // of tokens
 };
 
 struct NormRopeArgs {
@@ -97,6 +98,7 @@ struct NormRopeArgs {
   const float *cos_t, *sin_t;
   const int32_t* pos;    // [B][N] table rows, or null
   int rows;              // of the tables on a line
+  int past;              // store results past the caches
   int grid, F, Ht, Wd;   // grid: positions on the latent grid, tables of frames, rows and columns
 };
 
