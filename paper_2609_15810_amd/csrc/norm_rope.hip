@@ -82,8 +82,8 @@ __device__ __forceinline__ Lane lane_channels(int j, int rot) {
   if (LAYOUT == VC_ROPE_HALF) {
     const int rc = rot / 16;
     l.turn0 = l.turn1 = j < rc;
-    l.c0 = j < rc ? 8 * j : 16 * j;            // behind the turned part the pieces stand in order
-    l.c1 = j < rc ? 8 * (j + rc) : 16 * j + 8;
+    l.c0 = 8 * (j < rc ? j : j + rc);           // the pieces behind the turned part: the first half of them
+    l.c1 = 8 * (j < rc ? j + rc : j + G);       // in the first pieces, the others in the second
   } else {
     l.c0 = 8 * j;
     l.c1 = 8 * (j + G);
