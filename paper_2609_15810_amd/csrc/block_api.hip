@@ -145,7 +145,7 @@ size_t cross_args(const vc_cross_shape* s, const vc_cross_opts* o, bool backward
     if (!backward) a.part_ml = reinterpret_cast<float*>(part(a.splits * rows * 8));
   }
   if (backward) {
-    a.stats = reinterpret_cast<float*>(part((size_t)a.B * a.Hk * vc::cross_stat_rows(a.R) * 8));
+    a.stats = reinterpret_cast<float*>(part((size_t)a.B * a.Hq * vc::cross_stat_rows(a.M) * 8));
     if (a.row_splits > 1) a.part_kv = reinterpret_cast<float*>(part(a.row_splits * 2 * keys * a.d * 4));
   }
   return end;

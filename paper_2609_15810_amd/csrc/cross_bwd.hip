@@ -17,6 +17,8 @@
 // delta is sum_c dO_ic O_ic with O as the forward pass rounded it, an error of half a step of O per term. Where all keys of a
 // batch item are in one tile, it is formed from P and dP instead, which cancels exactly in dS where a row has few
 // keys (with one key dS is 0).
+#include <type_traits>
+
 #include "cross_common.hpp"
 
 namespace vc {
@@ -29,29 +31,8 @@ constexpr int KT = 64;         // keys of its tiles
 constexpr int KB = 32 * NW;    // keys of a workgroup of cross_dkv
 constexpr int RT = 32;         // rows of its tiles
 
-// rows of the row statistics per key head: whole workgroups of cross_dq
-__host__ __device__ __forceinline__ int64_t stat_rows(int R) { return ((int64_t)R + QR - 1) / QR * QR; }
-
-// A wave's 32 rows of D channels held as 32x32 results (column = row), times f: through its part of LDS, so that each
-// row is stored as a whole. dst(r) is row r's address, or null.
-template <int DT, int D, typename F>
-__device__ __forceinline__ void store_rows(const v16f (&o)[D / 32], float f, uint8_t* lds, int lane, F dst) {
-  using T = Tile<D>;
-  const int col = lane & 31, kh = lane >> 5;
-#pragma unroll
-  for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-    for (int g = 0; g < 4; ++g)
-      *reinterpret_cast<u2*>(lds + T::at(col, 4 * db + g) + 8 * kh) =
-          u2{pack2<DT>(o[db][4 * g] * f, o[db][4 * g + 1] * f), pack2<DT>(o[db][4 * g + 2] * f, o[db][4 * g + 3] * f)};
-  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-#pragma unroll
-  for (int u = 0; u < 32 / T::ROWS_PER_COPY; ++u) {
-    const int r = u * T::ROWS_PER_COPY + lane / T::CH, ch = lane % T::CH;
-    uint16_t* p = dst(r);
-    if (p) *reinterpret_cast<u4*>(p + 8 * ch) = *reinterpret_cast<const u4*>(lds + T::at(r, ch));
-  }
-}
+// rows of a query head's statistics: whole tiles of cross_dkv
+__host__ __device__ __forceinline__ int stat_rows(int M) { return (M + RT - 1) / RT * RT; }
 
 template <int DT>
 __device__ __forceinline__ float dot8(u4 a, u4 b, float s) {
@@ -79,11 +60,14 @@ __device__ __forceinline__ u4 pack_half(const v16f& s, int h) {
   return r;
 }
 
-template <int DT, int D, bool IDX, bool SPLIT>
+// GATHER: addresses per key (the keys are those of a list, or their stride is too far for one buffer); SPLIT: leave parts
+template <int DT, int D, bool GATHER, bool SPLIT>
 __global__ __launch_bounds__(64 * NW, 2) void cross_dq(CrossArgs a) {
   using T = Tile<D>;
-  constexpr int TB = KT * T::ROW, COPIES = KT / T::ROWS_PER_COPY / NW, KS = D / 16, DB = D / 32;
-  __shared__ __attribute__((aligned(16))) uint8_t kt[2][TB], vt[2][TB];
+  using C = Copier<D, KT, NW>;
+  constexpr int TB = KT * T::ROW, KS = D / 16, DB = D / 32;
+  __shared__ __attribute__((aligned(16))) uint8_t kt[4][TB];   // two tiles of K, two of V
+  uint8_t(*const vt)[TB] = kt + 2;
 
   const uint32_t wg = xcd_order(blockIdx.x, gridDim.x), blocks = (uint32_t)(a.R + QR - 1) / QR;
   const uint32_t rest = wg / blocks, bh = rest / (uint32_t)a.splits;
@@ -97,25 +81,30 @@ __global__ __launch_bounds__(64 * NW, 2) void cross_dq(CrossArgs a) {
 
   const uint16_t *kbase = a.K.p + b * a.K.sb + hk * a.K.sh, *vbase = a.V.p + b * a.V.sb + hk * a.V.sh;
   const int crow = lane / T::CH;
-  int next[COPIES];
+  const C kc(a.K.sn, wave, lane), vc(a.V.sn, wave, lane);
+  int next[C::COPIES];
   auto fetch = [&](int t) __attribute__((always_inline)) {
-    if (IDX) {
+    if (GATHER) {
 #pragma unroll
-      for (int u = 0; u < COPIES; ++u) {
+      for (int u = 0; u < C::COPIES; ++u) {
         const int j = k0 + t * KT + (u * NW + wave) * T::ROWS_PER_COPY + crow;
-        next[u] = j < k1 ? a.idx[(size_t)b * a.N + j] : -1;
+        next[u] = j < k1 ? (a.idx ? a.idx[(size_t)b * a.N + j] : j) : -1;
       }
     }
   };
   auto copy_tile = [&](int t, int buf) __attribute__((always_inline)) {
+    if (GATHER) {
 #pragma unroll
-    for (int u = 0; u < COPIES; ++u) {
-      const int q = u * NW + wave, r = q * T::ROWS_PER_COPY + crow;
-      const int j = k0 + t * KT + r, ch = (lane % T::CH) ^ T::key(r);
-      const int64_t src = IDX ? next[u] : j;
-      const bool in = IDX ? next[u] >= 0 : j < k1;
-      copy16(in ? (const void*)(kbase + src * a.K.sn + 8 * ch) : (const void*)&zero16, kt[buf] + q * 1024);
-      copy16(in ? (const void*)(vbase + src * a.V.sn + 8 * ch) : (const void*)&zero16, vt[buf] + q * 1024);
+      for (int u = 0; u < C::COPIES; ++u) {
+        const int q = u * NW + wave, ch = (lane % T::CH) ^ T::key(q * T::ROWS_PER_COPY + crow);
+        const int64_t src = next[u];
+        copy16(src >= 0 ? (const void*)(kbase + src * a.K.sn + 8 * ch) : (const void*)&zero16, kt[buf] + q * 1024);
+        copy16(src >= 0 ? (const void*)(vbase + src * a.V.sn + 8 * ch) : (const void*)&zero16, vt[buf] + q * 1024);
+      }
+    } else {
+      const int j = k0 + t * KT;
+      kc.copy(kbase + j * a.K.sn, k1 - j, kt[buf], wave);
+      vc.copy(vbase + j * a.V.sn, k1 - j, vt[buf], wave);
     }
   };
   if (tiles > 0) {
@@ -142,63 +131,77 @@ __global__ __launch_bounds__(64 * NW, 2) void cross_dq(CrossArgs a) {
   }
   delta = half_sum(delta);
   const float l2 = a.lse[((size_t)b * a.Hq + qr.h) * a.M + qr.i] * 1.4426950408889634f;
+  const RowOperands<D> rows0(lane);
+  const ColOperands<D> cols0(lane);
   v16f acc[DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db) acc[db] = v16f{};
 
+  // S^T and dP^T of the 32 keys from row 32 x of a tile, of which `valid` count; S becomes P
+  auto products = [&](uint32_t at, int x, int valid, v16f& s, v16f& dp) __attribute__((always_inline)) {
+    const RowOperands<D> rows = rows0.move(lds_addr(kt[0]) + at);
+    s = v16f{};
+    dp = v16f{};
+#pragma unroll
+    for (int i = 0; i < KS; ++i) {
+      s = mma<DT>(rows.get(32 * x * T::ROW, i), q[i], s);
+      dp = mma<DT>(rows.get(2 * TB + 32 * x * T::ROW, i), g[i], dp);
+    }
+    issue_reads<6>();
+    issue_products<2 * KS - 6, 1>();
+    issue_products<6, 0>();
+    __builtin_amdgcn_sched_barrier(0);
+    if (valid < 32 * x + 32) mask_scores(s, valid - 32 * x, kh);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], a.c, -l2));
+  };
   for (int t = 0; t < tiles; ++t) {
-    wait_copies();
+    wait_copies<0>();
     barrier();
     if (t + 1 < tiles) {
       copy_tile(t + 1, (t + 1) & 1);
       fetch(t + 2);
     }
     if (!active) continue;
-    const uint8_t *kb = kt[t & 1], *vb = vt[t & 1];
-    v16f s[2], dp[2];
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      s[x] = v16f{};
-      dp[x] = v16f{};
-#pragma unroll
-      for (int i = 0; i < KS; ++i) {
-        s[x] = mma<DT>(T::rows(kb, 32 * x, i, lane), q[i], s[x]);
-        dp[x] = mma<DT>(T::rows(vb, 32 * x, i, lane), g[i], dp[x]);
-      }
-    }
     const int valid = k1 - k0 - t * KT;
-#pragma unroll
-    for (int x = 0; x < 2; ++x)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const bool in = 32 * x + 8 * (r >> 2) + 4 * kh + (r & 3) < valid;
-        s[x][r] = in ? __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][r], a.c, -l2)) : 0.f;
-      }
+    v16f s, dp;
     if (n <= KT) {
       float d = 0.f;
+#pragma unroll 1
+      for (int x = 0; x < 2; ++x) {
+        products(0, x, valid, s, dp);
 #pragma unroll
-      for (int x = 0; x < 2; ++x)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) d = __builtin_fmaf(s[x][r], dp[x][r], d);
+        for (int r = 0; r < 16; ++r) d = __builtin_fmaf(s[r], dp[r], d);
+      }
       delta = half_sum(d);
     }
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
+      products((t & 1) * TB, x, valid, s, dp);
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[x][r] *= dp[x][r] - delta;
+      for (int r = 0; r < 16; ++r) s[r] *= dp[r] - delta;
+      const u4 ds[2] = {pack_half<DT>(s, 0), pack_half<DT>(s, 1)};
+      __builtin_amdgcn_sched_barrier(0);
+      const ColOperands<D> cols = cols0.move(lds_addr(kt[0]) + (t & 1) * TB);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const u4 ds = pack_half<DT>(s[x], h);
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int db = 0; db < DB; ++db) acc[db] = mma<DT>(T::cols(kb, 32 * x + 16 * h, db, lane), ds, acc[db]);
-      }
+        for (int db = 0; db < DB; ++db) acc[db] = mma<DT>(cols.get((32 * x + 16 * h) * T::ROW, db), ds[h], acc[db]);
+      issue_reads<8>();
+      issue_products<2 * DB - 4, 2>();
+      issue_products<4, 0>();
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
 
-  // what cross_dkv needs of a row; rows behind the last get probabilities of 0
-  if (split == 0 && kh == 0)
-    *reinterpret_cast<float2*>(a.stats + 2 * (bh * stat_rows(a.R) + row)) =
-        row < a.R ? make_float2(l2, delta) : make_float2(INFINITY, 0.f);
+  // what cross_dkv needs of a row; the rows that fill a head's last tile get probabilities of 0
+  if (split == 0 && kh == 0 && row < a.R) {
+    const int fill = stat_rows(a.M);
+    float* st = a.stats + 2 * (((size_t)b * a.Hq + qr.h) * fill + qr.i);
+    *reinterpret_cast<float2*>(st) = make_float2(l2, delta);
+    if (qr.i == a.M - 1)
+      for (int i = 1; i < fill - qr.i; ++i) *reinterpret_cast<float2*>(st + 2 * i) = make_float2(INFINITY, 0.f);
+  }
   if (SPLIT) {
     if (row < a.R) {
       float* p = a.part_o + (((size_t)split * a.B * a.Hk + bh) * a.R + row) * D + 4 * kh;
@@ -211,19 +214,21 @@ __global__ __launch_bounds__(64 * NW, 2) void cross_dq(CrossArgs a) {
     }
     return;
   }
-  barrier();
-  store_rows<DT, D>(acc, a.scale, kt[0] + wave * 32 * T::ROW, lane, [&](int r) __attribute__((always_inline)) -> uint16_t* {
-    if (r0 + r >= a.R) return nullptr;
-    const QueryRow w = query_row(a, hk, r0 + r);
-    return a.dQ.p + b * a.dQ.sb + w.h * a.dQ.sh + w.i * a.dQ.sn;
-  });
+  store_row<DT, D>(acc, a.scale, row < a.R ? a.dQ.p + b * a.dQ.sb + qr.h * a.dQ.sh + qr.i * a.dQ.sn : nullptr, lane);
 }
 
-template <int DT, int D, bool SPLIT>
-__global__ __launch_bounds__(64 * NW, 1) void cross_dkv(CrossArgs a) {
+// The sums of a wave's 32 keys take half of its registers, their K operand an eighth; V of the workgroup's keys stands in LDS,
+// so that two waves fit a SIMD, of two workgroups that are not in step: one's products and the other's vector work overlap.
+// (One wave a SIMD with V in registers: the products then leave their results in accumulation registers, 32 to 96 copies a
+// step; 283 us for 12 heads of 32760 rows and 512 keys.)
+// FAR: addresses per row (the rows' stride is too far for one buffer); SPLIT: leave parts
+template <int DT, int D, bool FAR, bool SPLIT>
+__global__ __launch_bounds__(64 * NW, 2) void cross_dkv(CrossArgs a) {
   using T = Tile<D>;
-  constexpr int TB = RT * T::ROW, COPIES = RT / T::ROWS_PER_COPY / NW, KS = D / 16, DB = D / 32;
-  __shared__ __attribute__((aligned(16))) uint8_t qt[2][TB], gt[2][TB];
+  using C = Copier<D, RT, NW>;
+  constexpr int TB = RT * T::ROW, KS = D / 16, DB = D / 32;
+  // V of the keys; of two row tiles Q, then dO; their statistics
+  __shared__ __attribute__((aligned(256))) uint8_t vt[KB * T::ROW], tile[2][2 * TB];
   __shared__ __attribute__((aligned(16))) float st[2][2 * RT];
 
   const uint32_t wg = xcd_order(blockIdx.x, gridDim.x), blocks = (uint32_t)(a.N + KB - 1) / KB;
@@ -234,62 +239,83 @@ __global__ __launch_bounds__(64 * NW, 1) void cross_dkv(CrossArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = keys_of(a, b);
   if (SPLIT && block * KB >= n) return;   // the join writes the zeros of keys that do not count
-  const int r0 = SPLIT ? split * a.row_chunk : 0, r1 = SPLIT ? min(a.R, r0 + a.row_chunk) : a.R;
-  const int tiles = block * KB < n ? (r1 - r0 + RT - 1) / RT : 0;
+  // row tiles, each of one query head: tile x of head g is g * per_head + x
+  const int per_head = (a.M + RT - 1) / RT;
+  const int t0 = SPLIT ? split * a.row_chunk : 0, t1 = SPLIT ? min(a.G * per_head, t0 + a.row_chunk) : a.G * per_head;
+  const int tiles = block * KB < n ? t1 - t0 : 0;
 
-  const uint16_t *qbase = a.Q.p + b * a.Q.sb, *gbase = a.dO.p + b * a.dO.sb;
-  const float* stats = a.stats + 2 * bh * stat_rows(a.R);
-  const int crow = lane / T::CH;
-  auto copy_tile = [&](int t, int buf) __attribute__((always_inline)) {
+  const C qc(a.Q.sn, wave, lane), gc(a.dO.sn, wave, lane);
+  int head = hk * a.G + t0 / per_head, m0 = t0 % per_head * RT;   // of the next tile to copy
+  auto copy_tile = [&](int to) __attribute__((always_inline)) {
+    const uint16_t *q = a.Q.p + b * a.Q.sb + head * a.Q.sh + m0 * a.Q.sn;
+    const uint16_t *g = a.dO.p + b * a.dO.sb + head * a.dO.sh + m0 * a.dO.sn;
+    if (FAR) {
 #pragma unroll
-    for (int u = 0; u < COPIES; ++u) {
-      const int x = u * NW + wave, r = x * T::ROWS_PER_COPY + crow;
-      const int i = r0 + t * RT + r, ch = (lane % T::CH) ^ T::key(r);
-      const bool in = i < a.R;
-      const QueryRow w = query_row(a, hk, min(i, a.R - 1));
-      copy16(in ? (const void*)(qbase + w.h * a.Q.sh + w.i * a.Q.sn + 8 * ch) : (const void*)&zero16, qt[buf] + x * 1024);
-      copy16(in ? (const void*)(gbase + w.h * a.dO.sh + w.i * a.dO.sn + 8 * ch) : (const void*)&zero16, gt[buf] + x * 1024);
+      for (int u = 0; u < C::COPIES; ++u) {
+        const int x = u * NW + wave, r = x * T::ROWS_PER_COPY + lane / T::CH, ch = (lane % T::CH) ^ T::key(r);
+        const bool in = m0 + r < a.M;
+        copy16(in ? (const void*)(q + r * a.Q.sn + 8 * ch) : (const void*)&zero16, tile[to] + x * 1024);
+        copy16(in ? (const void*)(g + r * a.dO.sn + 8 * ch) : (const void*)&zero16, tile[to] + TB + x * 1024);
+      }
+    } else {
+      qc.copy(q, a.M - m0, tile[to], wave);
+      gc.copy(g, a.M - m0, tile[to] + TB, wave);
     }
-    // row chunks are multiples of the tile, so a tile's statistics are in the padded array
-    if (wave == 0 && lane < RT / 2) copy16(stats + 2 * (r0 + t * RT) + 4 * lane, st[buf]);
+    if (wave == 0 && lane < RT / 2)
+      copy16(a.stats + 2 * (((size_t)b * a.Hq + head) * stat_rows(a.M) + m0) + 4 * lane, st[to]);
+    m0 += RT;
+    if (m0 >= a.M) m0 = 0, ++head;
   };
-  if (tiles > 0) copy_tile(0, 0);
+  if (tiles > 0) copy_tile(0);
 
-  const int j = block * KB + 32 * wave + col;   // this lane's key, in the order of the list
+  // this lane's key, in the order of the list; its K in registers, its V in LDS in the place of row `col` of the wave's
+  const int j = block * KB + 32 * wave + col;
   const bool counts = j < n;
   const bool active = block * KB + 32 * wave < n;
   const int64_t key = j < a.N ? (a.idx ? a.idx[(size_t)b * a.N + j] : j) : 0;
-  u4 k[KS], v[KS];
+  u4 k[KS];
   {
     const uint16_t *pk = a.K.p + b * a.K.sb + hk * a.K.sh + key * a.K.sn + 8 * kh;
     const uint16_t *pv = a.V.p + b * a.V.sb + hk * a.V.sh + key * a.V.sn + 8 * kh;
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
       k[s] = counts ? *reinterpret_cast<const u4*>(pk + 16 * s) : u4{0, 0, 0, 0};
-      v[s] = counts ? *reinterpret_cast<const u4*>(pv + 16 * s) : u4{0, 0, 0, 0};
+      *reinterpret_cast<u4*>(vt + T::at(32 * wave + col, 2 * s + kh)) =
+          counts ? *reinterpret_cast<const u4*>(pv + 16 * s) : u4{0, 0, 0, 0};
     }
   }
   v16f dk[DB], dv[DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db) dk[db] = dv[db] = v16f{};
+  const RowOperands<D> vrows = RowOperands<D>(lane).move(lds_addr(vt) + 32 * wave * T::ROW);
+  RowOperands<D> rows = RowOperands<D>(lane).move(lds_addr(tile));
+  ColOperands<D> cols = ColOperands<D>(lane).move(lds_addr(tile));
+  const uint32_t st0 = lds_addr(st) + 32 * kh;
 
   for (int t = 0; t < tiles; ++t) {
-    wait_copies();
+    wait_copies<0>();
     barrier();
-    if (t + 1 < tiles) copy_tile(t + 1, (t + 1) & 1);
+    if (t + 1 < tiles) copy_tile((t + 1) & 1);
     if (!active) continue;
-    const uint8_t *qb = qt[t & 1], *gb = gt[t & 1];
     v16f s = {}, dp = {};
 #pragma unroll
     for (int i = 0; i < KS; ++i) {
-      s = mma<DT>(T::rows(qb, 0, i, lane), k[i], s);
-      dp = mma<DT>(T::rows(gb, 0, i, lane), v[i], dp);
+      s = mma<DT>(rows.get(0, i), k[i], s);
+      dp = mma<DT>(rows.get(TB, i), vrows.get(0, i), dp);
     }
+    issue_reads<6>();
+#pragma unroll
+    for (int i = 0; i < KS; ++i) {
+      issue_products<1, 1>();
+      issue_products<1, 2>();
+    }
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-      const float4 x = *reinterpret_cast<const float4*>(&st[t & 1][2 * (8 * g + 4 * kh)]);
-      const float4 y = *reinterpret_cast<const float4*>(&st[t & 1][2 * (8 * g + 4 * kh) + 4]);
-      const float l2[4] = {x.x, x.z, y.x, y.z}, dl[4] = {x.y, x.w, y.y, y.w};
+      typedef float f4 __attribute__((ext_vector_type(4)));
+      typedef const __attribute__((address_space(3))) f4* at;
+      const f4 x = *(at)(st0 + (t & 1) * 8 * RT + 64 * g), y = *(at)(st0 + (t & 1) * 8 * RT + 64 * g + 16);
+      const float l2[4] = {x[0], x[2], y[0], y[2]}, dl[4] = {x[1], x[3], y[1], y[3]};
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int r = 4 * g + e;
@@ -297,15 +323,23 @@ __global__ __launch_bounds__(64 * NW, 1) void cross_dkv(CrossArgs a) {
         dp[r] = s[r] * (dp[r] - dl[e]);
       }
     }
+    u4 p[2], ds[2];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const u4 p = pack_half<DT>(s, h), ds = pack_half<DT>(dp, h);
+    for (int h = 0; h < 2; ++h) p[h] = pack_half<DT>(s, h), ds[h] = pack_half<DT>(dp, h);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int db = 0; db < DB; ++db) {
-        dv[db] = mma<DT>(T::cols(gb, 16 * h, db, lane), p, dv[db]);
-        dk[db] = mma<DT>(T::cols(qb, 16 * h, db, lane), ds, dk[db]);
+        dv[db] = mma<DT>(cols.get(TB + 16 * h * T::ROW, db), p[h], dv[db]);
+        dk[db] = mma<DT>(cols.get(16 * h * T::ROW, db), ds[h], dk[db]);
       }
-    }
+    issue_reads<10>();
+    issue_products<4 * DB - 5, 2>();
+    issue_products<5, 0>();
+    __builtin_amdgcn_sched_barrier(0);
+    rows.shift((t & 1) ? -2 * TB : 2 * TB);
+    cols.shift((t & 1) ? -2 * TB : 2 * TB);
   }
 
   if (SPLIT) {
@@ -332,18 +366,11 @@ __global__ __launch_bounds__(64 * NW, 1) void cross_dkv(CrossArgs a) {
       dk[db][r] = counts ? dk[db][r] : 0.f;
       dv[db][r] = counts ? dv[db][r] : 0.f;
     }
-  barrier();
-  uint8_t* lds = (wave < 2 ? qt[wave] : gt[wave - 2]);
-  static_assert(TB >= 32 * T::ROW, "a wave's keys fit one row tile");
-  const int j0 = block * KB + 32 * wave;
-  auto row_of = [&](const Strided& t, int r) __attribute__((always_inline)) -> uint16_t* {
-    if (j0 + r >= a.N) return nullptr;
-    const int64_t i = a.idx ? a.idx[(size_t)b * a.N + j0 + r] : j0 + r;
-    return t.p + b * t.sb + hk * t.sh + i * t.sn;
+  auto row_of = [&](const Strided& t) __attribute__((always_inline)) -> uint16_t* {
+    return j < a.N ? t.p + b * t.sb + hk * t.sh + key * t.sn : nullptr;
   };
-  store_rows<DT, D>(dk, a.scale, lds, lane, [&](int r) __attribute__((always_inline)) { return row_of(a.dK, r); });
-  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-  store_rows<DT, D>(dv, 1.f, lds, lane, [&](int r) __attribute__((always_inline)) { return row_of(a.dV, r); });
+  store_row<DT, D>(dk, a.scale, row_of(a.dK), lane);
+  store_row<DT, D>(dv, 1.f, row_of(a.dV), lane);
 }
 
 // Sums of parts [part][row][D] at p (rows * D apart by `step`): as cross_join, d / 4 lanes and `groups` of them a row;
@@ -410,23 +437,27 @@ hipError_t backward(const CrossArgs& a, hipStream_t s) {
   const int64_t heads = (int64_t)a.B * a.Hk;
   const unsigned gq = (unsigned)((int64_t)(a.R + QR - 1) / QR * heads * a.splits);
   const unsigned gk = (unsigned)((int64_t)(a.N + KB - 1) / KB * heads * a.row_splits);
+  const bool gather = a.idx || a.K.sn >= FAR_STRIDE || a.V.sn >= FAR_STRIDE;
+  const bool far = a.Q.sn >= FAR_STRIDE || a.dO.sn >= FAR_STRIDE;
   hipError_t e;
   if (a.splits > 1) {
-    if (a.idx) cross_dq<DT, D, true, true><<<gq, 64 * NW, 0, s>>>(a);
+    if (gather) cross_dq<DT, D, true, true><<<gq, 64 * NW, 0, s>>>(a);
     else cross_dq<DT, D, false, true><<<gq, 64 * NW, 0, s>>>(a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     cross_join_dq<DT, D><<<(unsigned)((heads * a.R + jq - 1) / jq), 256, 0, s>>>(a, gj);
   } else {
-    if (a.idx) cross_dq<DT, D, true, false><<<gq, 64 * NW, 0, s>>>(a);
+    if (gather) cross_dq<DT, D, true, false><<<gq, 64 * NW, 0, s>>>(a);
     else cross_dq<DT, D, false, false><<<gq, 64 * NW, 0, s>>>(a);
   }
   if ((e = hipGetLastError()) != hipSuccess) return e;
   if (a.row_splits > 1) {
-    cross_dkv<DT, D, true><<<gk, 64 * NW, 0, s>>>(a);
+    if (far) cross_dkv<DT, D, true, true><<<gk, 64 * NW, 0, s>>>(a);
+    else cross_dkv<DT, D, false, true><<<gk, 64 * NW, 0, s>>>(a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     cross_join_dkv<DT, D><<<dim3((unsigned)((heads * a.N + jk - 1) / jk), 2), 256, 0, s>>>(a, gkj);
   } else {
-    cross_dkv<DT, D, false><<<gk, 64 * NW, 0, s>>>(a);
+    if (far) cross_dkv<DT, D, true, false><<<gk, 64 * NW, 0, s>>>(a);
+    else cross_dkv<DT, D, false, false><<<gk, 64 * NW, 0, s>>>(a);
   }
   return hipGetLastError();
 }
@@ -437,16 +468,16 @@ hipError_t backward(const CrossArgs& a, hipStream_t s) {
 void cross_plan_backward(CrossArgs& a) {
   using namespace cross;
   cross_plan(a);
-  // rows are split where the keys alone do not give every CU a workgroup
-  const int64_t base = (int64_t)(a.N + KB - 1) / KB * a.B * a.Hk, tiles = ((int64_t)a.R + RT - 1) / RT;
-  int64_t splits = base >= 256 ? 1 : 256 / base;
+  // row tiles are split where the keys alone do not give every CU two workgroups
+  const int64_t base = (int64_t)(a.N + KB - 1) / KB * a.B * a.Hk, tiles = (int64_t)a.G * ((a.M + RT - 1) / RT);
+  int64_t splits = base >= 256 ? 1 : 512 / base;
   if (splits > tiles) splits = tiles;
   const int64_t per = (tiles + splits - 1) / splits;
-  a.row_chunk = (int)(per * RT);
+  a.row_chunk = (int)per;
   a.row_splits = (int)((tiles + per - 1) / per);
 }
 
-int64_t cross_stat_rows(int R) { return cross::stat_rows(R); }
+int cross_stat_rows(int M) { return cross::stat_rows(M); }
 
 hipError_t launch_cross_backward(const CrossArgs& a, hipStream_t s) {
   if (a.d == 128) return a.dtype == VC_BF16 ? cross::backward<VC_BF16, 128>(a, s) : cross::backward<VC_FP16, 128>(a, s);

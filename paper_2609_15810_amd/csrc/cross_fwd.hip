@@ -14,6 +14,8 @@
 //
 // Few rows and long keys: the keys are split over workgroups (cross_plan), each leaves unnormalised fp32 outputs with its
 // maximum and sum, and cross_join adds them up in a fixed order.
+#include <type_traits>
+
 #include "cross_common.hpp"
 
 namespace vc {
@@ -28,6 +30,18 @@ constexpr int KT = 64;          // keys of a tile
 // units): it moves, and the sums are rescaled, only where the maximum has left it by more. Probabilities then reach 2^LAG,
 // which the 16-bit types and the fp32 sums hold with the same relative errors.
 constexpr float LAG = 8.f;
+
+// A lane's row: O = o / l and lse
+template <int DT, int D>
+__device__ __forceinline__ void finish_row(const CrossArgs& a, int b, int hk, int row, int n, const v16f (&o)[D / 32], float m,
+                                           float l, int lane) {
+  const QueryRow w = query_row(a, hk, min(row, a.R - 1));
+  // no key counts: O = 0, lse = -inf
+  const float inv = n > 0 ? 1.f / l : 0.f;
+  if (a.lse && row < a.R && lane < 32)
+    a.lse[((size_t)b * a.Hq + w.h) * a.M + w.i] = n > 0 ? (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : -INFINITY;
+  store_row<DT, D>(o, inv, row < a.R ? a.O.p + b * a.O.sb + w.h * a.O.sh + w.i * a.O.sn : nullptr, lane);
+}
 
 // GATHER: addresses per key (the keys are those of a list, or their stride is too far for one buffer);
 // SPLIT: leave parts
@@ -95,6 +109,8 @@ __global__ __launch_bounds__(64 * NW, 2) void cross_fwd(CrossArgs a) {
   v16f o[DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db) o[db] = v16f{};
+  const RowOperands<D> rows0(lane);
+  const ColOperands<D> cols0(lane);
   float m = -INFINITY, l = 0.f;   // the reference; the sum of this lane's keys
 
   for (int t = 0; t < tiles; ++t) {
@@ -105,23 +121,21 @@ __global__ __launch_bounds__(64 * NW, 2) void cross_fwd(CrossArgs a) {
       fetch(t + 2);
     }
     if (!active) continue;
-    const uint8_t *kb = kt[t & 1], *vb = vt[t & 1];
+    const RowOperands<D> rows = rows0.move(lds_addr(kt[0]) + (t & 1) * TB);
+    const ColOperands<D> cols = cols0.move(lds_addr(vt[0]) + (t & 1) * TB);
     v16f s[2];
 #pragma unroll
     for (int g = 0; g < 2; ++g) s[g] = v16f{};
 #pragma unroll
     for (int i = 0; i < KS; ++i)
 #pragma unroll
-      for (int g = 0; g < 2; ++g) s[g] = mma<DT>(T::rows(kb, 32 * g, i, lane), q[i], s[g]);
+      for (int g = 0; g < 2; ++g) s[g] = mma<DT>(rows.get(32 * g * T::ROW, i), q[i], s[g]);
+    issue_reads<6>();
+    issue_products<2 * KS - 6, 1>();
+    issue_products<6, 0>();
+    __builtin_amdgcn_sched_barrier(0);
     const int valid = k1 - k0 - t * KT;
-    if (valid < KT) {
-      asm volatile("");   // a branch, taken once at most, and not 32 selections in every tile
-#pragma unroll
-      for (int g = 0; g < 2; ++g)
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (32 * g + 8 * (r >> 2) + 4 * kh + (r & 3) >= valid) s[g][r] = -INFINITY;
-    }
+    if (valid < KT) mask_scores(s, valid, kh);
     float top = fmaxf(s[0][0], s[1][0]);
 #pragma unroll
     for (int r = 1; r < 16; ++r) top = fmaxf(fmaxf(top, s[0][r]), s[1][r]);
@@ -148,7 +162,7 @@ __global__ __launch_bounds__(64 * NW, 2) void cross_fwd(CrossArgs a) {
         }
         const u4 pp = {pack2<DT>(p[0], p[1]), pack2<DT>(p[2], p[3]), pack2<DT>(p[4], p[5]), pack2<DT>(p[6], p[7])};
 #pragma unroll
-        for (int db = 0; db < DB; ++db) o[db] = mma<DT>(T::cols(vb, 32 * g + 16 * h, db, lane), pp, o[db]);
+        for (int db = 0; db < DB; ++db) o[db] = mma<DT>(cols.get((32 * g + 16 * h) * T::ROW, db), pp, o[db]);
       }
   }
   l = half_sum(l);
@@ -167,29 +181,217 @@ __global__ __launch_bounds__(64 * NW, 2) void cross_fwd(CrossArgs a) {
     }
     return;
   }
-  // no key counts: O = 0, lse = -inf
-  const float inv = n > 0 ? 1.f / l : 0.f;
-  if (a.lse && row < a.R && kh == 0)
-    a.lse[((size_t)b * a.Hq + qr.h) * a.M + qr.i] = n > 0 ? (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : -INFINITY;
-  // rows leave through LDS, so that each is stored as a whole
-  barrier();
-  uint8_t* out = kt[0] + wave * 32 * T::ROW;
-  static_assert(NW * 32 <= 2 * KT, "a workgroup's rows fit the two key buffers");
+  finish_row<DT, D>(a, b, hk, row, n, o, m, l, lane);
+}
+
+// Many rows: a workgroup on each CU, of eight waves of 32 rows that share the tiles, two on each SIMD, in two groups that are
+// half a step apart: while one group's waves issue products (the values of a tile, then the scores of the next), those of
+// the other form probabilities; a barrier ends each half step, so that the matrix cores always have one group's products.
+// The workgroup walks over blocks of 256 rows of a query head, those of a head without a break: their tiles are one sequence,
+// copied two steps ahead (pair g: K of tile g and V of tile g - 1, both first read by the products of step g), the next
+// block's queries are copied into LDS a block ahead, and a block's rows are stored in the first step of the next.
+constexpr int WW = 8;           // waves
+constexpr int WR = 32 * WW;     // rows of a block
+constexpr int RING = 3;         // tiles of K and of V in LDS
+
+template <int DT, int D, bool GATHER>
+__global__ __launch_bounds__(64 * WW, 2) void cross_fwd_wide(CrossArgs a, int total) {
+  using T = Tile<D>;
+  using C = Copier<D, KT, WW>;
+  constexpr int TB = KT * T::ROW, KS = D / 16, DB = D / 32;
+  __shared__ __attribute__((aligned(16))) uint8_t kt[RING][TB], vt[RING][TB], qt[WR * T::ROW];
+
+  const int blocks = (a.M + WR - 1) / WR;   // of a query head
+  const uint32_t wg = xcd_order(blockIdx.x, gridDim.x);
+  const int end = (int)((int64_t)total * (wg + 1) / gridDim.x);
+  const int lane = threadIdx.x & 63, col = lane & 31, kh = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const bool late = wave >= WW / 2;
+  const C kc(a.K.sn, wave, lane), vc(a.V.sn, wave, lane);
+
+  uint8_t* const mine = qt + wave * 32 * T::ROW;   // this wave's queries of the next block
+
+  for (int block = (int)((int64_t)total * wg / gridDim.x); block < end;) {
+    // the blocks of one query head from here on
+    const uint32_t bh = block / (uint32_t)blocks;
+    const int b = bh / (uint32_t)a.Hq, h = bh - b * a.Hq;
+    const int rb = block - bh * blocks, count = min(end - block, blocks - rb);
+    block += count;
+    const int n = __builtin_amdgcn_readfirstlane(keys_of(fresh_args(), b)), tiles = (n + KT - 1) / KT;
+
+    u4 q[KS], p[4];
+    v16f o[DB], s[2];
+    float m = -INFINITY, l = 0.f;   // the reference; the sum of this lane's keys
+    // The rows of a finished block; the sums start anew where the reference is -inf. As many stores in every call: one per
+    // piece of a row and one of lse.
+    constexpr int STORES = D / 16;
+    auto finish = [&](int x) __attribute__((always_inline)) {
+      const CrossArgs f = fresh_args();
+      const int r0 = (rb + x) * WR, rows = min(WR, f.M - r0);
+      const float sum = half_sum(l), inv = n > 0 ? 1.f / sum : 0.f;
+      const auto out = buffer_of(f.O.p + b * f.O.sb + h * f.O.sh + r0 * f.O.sn, (uint32_t)(rows - 1) * 2 * f.O.sn + 2 * D);
+      const int at = (32 * wave + col) * 2 * (int)f.O.sn;
+      row_pieces<DT, D>(o, inv, lane, [&](int c, u4 w) __attribute__((always_inline)) {
+        __builtin_amdgcn_raw_buffer_store_b128(w, out, at + 2 * c, 0, 0);
+      });
+      // (without an lse: a buffer of no bytes)
+      const auto lse = buffer_of(f.lse ? f.lse + ((size_t)b * f.Hq + h) * f.M + r0 : nullptr, f.lse ? 4 * rows : 0);
+      const float value = n > 0 ? (m + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f : -INFINITY;
+      __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(value), lse, 4 * (32 * wave + col), 0, 0);
+      m = -INFINITY;
+    };
+    if (n == 0) {
 #pragma unroll
-  for (int db = 0; db < DB; ++db)
-#pragma unroll
-    for (int g = 0; g < 4; ++g)
-      *reinterpret_cast<u2*>(out + T::at(col, 4 * db + g) + 8 * kh) =
-          u2{pack2<DT>(o[db][4 * g] * inv, o[db][4 * g + 1] * inv), pack2<DT>(o[db][4 * g + 2] * inv, o[db][4 * g + 3] * inv)};
-  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-#pragma unroll
-  for (int u = 0; u < 32 / T::ROWS_PER_COPY; ++u) {
-    const int r = u * T::ROWS_PER_COPY + crow, ch = lane % T::CH;
-    if (r0 + r < a.R) {
-      const QueryRow w = query_row(a, hk, r0 + r);
-      *reinterpret_cast<u4*>(a.O.p + b * a.O.sb + w.h * a.O.sh + w.i * a.O.sn + 8 * ch) =
-          *reinterpret_cast<const u4*>(out + T::at(r, ch));
+      for (int db = 0; db < DB; ++db) o[db] = v16f{};
+      for (int x = 0; x < count; ++x) finish(x);
+      continue;
     }
+
+    const CrossArgs f = fresh_args();
+    const uint32_t hk = (uint32_t)h / (uint32_t)f.G;
+    const uint16_t *kbase = f.K.p + b * f.K.sb + hk * f.K.sh, *vbase = f.V.p + b * f.V.sb + hk * f.V.sh;
+    auto copy_one = [&](const uint16_t* base, int64_t sn, const C& c, int t, uint8_t* to) __attribute__((always_inline)) {
+      if (GATHER) {
+#pragma unroll
+        for (int u = 0; u < C::COPIES; ++u) {
+          const int x = u * WW + wave, r = x * T::ROWS_PER_COPY + lane / T::CH, j = t * KT + r;
+          const int64_t src = j < n ? (a.idx ? a.idx[(size_t)b * a.N + j] : j) : -1;
+          copy16(src >= 0 ? (const void*)(base + src * sn + 8 * ((lane % T::CH) ^ T::key(r))) : (const void*)&zero16,
+                 to + x * 1024);
+        }
+      } else {
+        c.copy(base + (int64_t)t * KT * sn, n - t * KT, to, wave);
+      }
+    };
+    // the next pair to copy: K of tile `ahead` of a block, of `left` blocks still to come; V of tile `behind`
+    int left = count, pair = 0, ahead = 0, behind = -1;
+    auto copy_pair = [&]() __attribute__((always_inline)) {
+      if (behind >= 0) copy_one(vbase, a.V.sn, vc, behind, vt[(pair + RING - 1) % RING]);
+      behind = -1;
+      if (left > 0) {
+        copy_one(kbase, a.K.sn, kc, ahead, kt[pair % RING]);
+        behind = ahead;
+        ++ahead;
+        if (ahead == tiles) ahead = 0, --left;
+      }
+      pair = (pair + 1) % RING;
+    };
+    // this wave's queries of block x: on their way into LDS, and from there
+    auto copy_queries = [&](int x) __attribute__((always_inline)) {
+      const CrossArgs f = fresh_args();
+      const int r0 = (rb + x) * WR + 32 * wave;
+      int l = lane;
+      lanes::pin(l);   // (seldom: its addresses are not to be held)
+      Copier<D, 32, 1>(f.Q.sn, 0, l).copy(f.Q.p + b * f.Q.sb + h * f.Q.sh + r0 * f.Q.sn, f.M - r0, mine, 0);
+    };
+    auto load_queries = [&]() __attribute__((always_inline)) {
+      wait_copies<0>();
+      int l = lane;
+      lanes::pin(l);
+      const RowOperands<D> at = RowOperands<D>(l).move(lds_addr(mine));
+#pragma unroll
+      for (int s = 0; s < KS; ++s) q[s] = at.get(0, s);
+#pragma unroll
+      for (int s = 0; s < KS; ++s) lanes::pin(q[s]);
+    };
+    // operands of the tile whose scores, and of that whose values come next
+    RowOperands<D> rows = RowOperands<D>(lane).move(lds_addr(kt[0]));
+    ColOperands<D> cols = ColOperands<D>(lane).move(lds_addr(vt[0]));
+    auto scores = [&]() __attribute__((always_inline)) {
+#pragma unroll
+      for (int x = 0; x < 2; ++x) s[x] = v16f{};
+#pragma unroll
+      for (int i = 0; i < KS; ++i)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) s[x] = mma<DT>(rows.get(32 * x * T::ROW, i), q[i], s[x]);
+    };
+    auto values = [&]() __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int db = 0; db < DB; ++db) o[db] = mma<DT>(cols.get(16 * i * T::ROW, db), p[i], o[db]);
+    };
+    auto probabilities = [&](int valid) __attribute__((always_inline)) {
+      if (valid < KT) mask_scores(s, valid, kh);
+      float top = fmaxf(s[0][0], s[1][0]);
+#pragma unroll
+      for (int r = 1; r < 16; ++r) top = fmaxf(fmaxf(top, s[0][r]), s[1][r]);
+      top = half_max(top) * a.c;
+      if (__builtin_amdgcn_ballot_w64(top > m + LAG)) {
+        const float up = top > m + LAG ? top : m, alpha = __builtin_amdgcn_exp2f(m - (up == -INFINITY ? 0.f : up));
+        const bool anew = m == -INFINITY;   // (selected, not multiplied: what stands there may not be finite)
+        m = up;
+        l = anew ? 0.f : l * alpha;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[db][r] = anew ? 0.f : o[db][r] * alpha;
+      }
+      const float off = m == -INFINITY ? 0.f : m;   // scores of -inf alone so far
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float e[8];
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+          e[x] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i >> 1][8 * (i & 1) + x], a.c, -off));
+          l += e[x];
+        }
+        p[i] = u4{pack2<DT>(e[0], e[1]), pack2<DT>(e[2], e[3]), pack2<DT>(e[4], e[5]), pack2<DT>(e[6], e[7])};
+      }
+    };
+
+    copy_queries(0);
+    for (int x = 0; x < RING - 1; ++x) copy_pair();
+    load_queries();
+    if (count > 1) copy_queries(1);
+    barrier();
+    if (late) barrier();
+    scores();
+    barrier();
+    int slot = 0, x = 0, t = 0;   // of the tile at work: its place in the ring, its block, its place in the block
+    rows.shift(TB);
+    bool stored = false;
+    for (;;) {
+      // probabilities
+      copy_pair();
+      if (stored) finish(x - 1);   // the block before the one at work is complete
+      const bool last = t + 1 == tiles;
+      probabilities(n - t * KT);
+      if (last && x + 1 < count) {
+        load_queries();
+        if (x + 2 < count) copy_queries(x + 2);
+      }
+      barrier();
+      if (last && x + 1 == count) break;
+      // products: values of this tile, scores of the next
+      
+      values();
+      scores();
+      // operands are read six products ahead of their use
+      issue_reads<12>();
+      issue_products<4 * DB - 6, 2>();
+      issue_products<6, 1>();
+      issue_products<2 * KS - 6, 1>();
+      issue_products<6, 0>();
+      
+      cols.shift(slot < RING - 1 ? TB : -(RING - 1) * TB);
+      slot = slot + 1 < RING ? slot + 1 : 0;
+      rows.shift(slot < RING - 1 ? TB : -(RING - 1) * TB);
+      // the next pair is there; rows that were stored behind it may be on their way
+      if (stored && !last) wait_copies<STORES + 1>();
+      else wait_copies<0>();
+      barrier();
+      stored = last;
+      ++t;
+      if (last) {
+        ++x;
+        t = 0;
+      }
+    }
+    values();
+    finish(x);
+    if (!late) barrier();   // the groups meet again
+    barrier();              // and the tiles are read no more
   }
 }
 
@@ -277,7 +479,11 @@ template <int DT, int D>
 hipError_t forward(const CrossArgs& a, hipStream_t s) {
   const unsigned grid = (unsigned)((int64_t)(a.R + QR - 1) / QR * a.B * a.Hk * a.splits);
   const bool gather = a.idx || a.K.sn >= FAR_STRIDE || a.V.sn >= FAR_STRIDE;
-  if (a.splits > 1) {
+  const int wide = (int)((int64_t)(a.M + WR - 1) / WR * a.B * a.Hq);
+  if (a.splits == 1 && wide >= 256 && a.M >= WR && a.Q.sn < FAR_STRIDE && a.O.sn < FAR_STRIDE) {
+    if (gather) cross_fwd_wide<DT, D, true><<<256, 64 * WW, 0, s>>>(a, wide);
+    else cross_fwd_wide<DT, D, false><<<256, 64 * WW, 0, s>>>(a, wide);
+  } else if (a.splits > 1) {
     if (gather) cross_fwd<DT, D, true, true><<<grid, 64 * NW, 0, s>>>(a);
     else cross_fwd<DT, D, false, true><<<grid, 64 * NW, 0, s>>>(a);
     const hipError_t e = hipGetLastError();
@@ -302,10 +508,11 @@ hipError_t launch_cross_keys(const uint8_t* k_mask, int64_t stride, const int32_
 
 void cross_plan(CrossArgs& a) {
   using namespace cross;
-  // keys are split where the rows alone do not give every CU two workgroups
+  // Keys are split where the rows alone do not give every CU two workgroups, and only where that shortens a workgroup's walk
+  // by more than the joining launch costs: a tile takes 1.3 us alone, the join 4 to 5 us
   const int64_t base = (int64_t)(a.R + QR - 1) / QR * a.B * a.Hk;
   const int64_t tiles = (a.N + KT - 1) / KT;
-  int64_t splits = base >= 256 ? 1 : (512 + base - 1) / base;
+  int64_t splits = base >= 256 || tiles <= 4 ? 1 : (512 + base - 1) / base;
   if (splits > tiles) splits = tiles;
   const int64_t per = (tiles + splits - 1) / splits;
   a.chunk = (int)(per * KT);

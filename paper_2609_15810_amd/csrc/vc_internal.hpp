@@ -124,8 +124,8 @@ struct CrossArgs {
   float* part_o;         // [splits][B Hk][R][d] unnormalised outputs (backward: parts of dQ)
   float* part_ml;        // [splits][B Hk][R][2] running maximum (log2 units) and sum
   // backward
-  float* stats;          // [B Hk][R rounded up to workgroups][2] lse in log2 units and delta
-  int row_splits, row_chunk;   // rows split over workgroups that form dK and dV
+  float* stats;          // [B][Hq][cross_stat_rows(M)][2] lse in log2 units and delta
+  int row_splits, row_chunk;   // row tiles split over workgroups that form dK and dV
   float* part_kv;        // [row_splits][2][B Hk][N][d] parts of dK and dV
 };
 
@@ -146,7 +146,7 @@ hipError_t launch_cross_keys(const uint8_t* k_mask, int64_t stride, const int32_
 // How a call's keys are split (a.splits, a.chunk), and for the backward pass its rows (a.row_splits, a.row_chunk)
 void cross_plan(CrossArgs& a);
 void cross_plan_backward(CrossArgs& a);
-int64_t cross_stat_rows(int R);
+int cross_stat_rows(int M);   // rows of a query head's statistics
 hipError_t launch_cross_forward(const CrossArgs& a, hipStream_t s);
 hipError_t launch_cross_backward(const CrossArgs& a, hipStream_t s);
 

@@ -140,6 +140,16 @@ def test_many_rows_at_once():
     near(out[:, :, at.cuda()], ref.O, ref.O_err, "O")
 
 
+@pytest.mark.parametrize("B,Hq,Hk,M,N,d,dtype,mask", [
+    (2, 12, 4, 2900, 130, 128, BF, "both"),     # grouped heads, ragged lists, an item without a key
+    (1, 24, 24, 2817, 64, 128, FP, "none"),     # one tile a block
+    (3, 8, 8, 2570, 201, 64, BF, "len"), (2, 16, 2, 2305, 1, 64, FP, "none"), (4, 40, 40, 300, 70, 128, BF, "mask"),
+    (1, 300, 300, 257, 65, 64, BF, "none")])
+def test_blocks_of_many_rows(B, Hq, Hk, M, N, d, dtype, mask):
+    """enough blocks of 256 rows for the kernel that walks over them: ends of heads, of blocks and of the work of a CU"""
+    Problem(B, Hq, Hk, M, N, d, dtype, mask).check(backward=False)
+
+
 @pytest.mark.parametrize("scale", [0.02, 0.5])
 def test_scale(scale):
     Problem(1, 2, 2, 50, 90, scale=scale).check()
@@ -175,6 +185,22 @@ def test_offsets_beyond_32_bits():
     op.forward(q5, kk, p.V, near_o)
     op.forward(q5, kk, p.V, out)
     assert torch.equal(out, near_o)
+
+
+def test_rows_far_apart():
+    # strides of queries and of their gradients that one buffer does not reach over a tile
+    p = Problem(1, 2, 1, 70, 40)
+    ref, lse = p.forward()
+    grads = p.backward(ref, lse)
+    wide = torch.empty((3, 70, 1 << 22), dtype=BF, device="cuda")
+    far = [wide[i].as_strided((1, 2, 70, 128), (256, 128, 1 << 22, 1), wide[i].storage_offset()) for i in range(3)]
+    far[0].copy_(p.Q)
+    far[1].copy_(p.dO)
+    p.Q, p.dO = far[0], far[1]
+    out, lse2 = p.forward()
+    assert torch.equal(out, ref) and torch.equal(lse2, lse)
+    far[2].copy_(out)
+    assert all(torch.equal(a, b) for a, b in zip(p.backward(far[2], lse), grads))
 
 
 def test_reproducible():
