@@ -512,9 +512,10 @@ void cross_plan(CrossArgs& a) {
   // by more than the joining launch costs: a tile takes 1.3 us alone, the join 4 to 5 us
   const int64_t base = (int64_t)(a.R + QR - 1) / QR * a.B * a.Hk;
   const int64_t tiles = (a.N + KT - 1) / KT;
-  int64_t splits = base >= 256 || tiles <= 4 ? 1 : (512 + base - 1) / base;
+  int64_t splits = base >= 256 ? 1 : (512 + base - 1) / base;
   if (splits > tiles) splits = tiles;
-  const int64_t per = (tiles + splits - 1) / splits;
+  int64_t per = (tiles + splits - 1) / splits;
+  if (tiles - per < 5) per = tiles;
   a.chunk = (int)(per * KT);
   a.splits = (int)((tiles + per - 1) / per);
 }
