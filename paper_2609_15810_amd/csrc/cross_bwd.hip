@@ -14,9 +14,10 @@
 // order for the next product, whose other operand is read from LDS by transposing reads. P and dS are rounded to the
 // operands' 16 bits, as the matrix instructions take them; sums are fp32.
 //
-// delta is sum_c dO_ic O_ic with O as the forward pass rounded it, an error of half a step of O per term. Where all keys of a
-// batch item are in one tile, it is formed from P and dP instead, which cancels exactly in dS where a row has few
-// keys (with one key dS is 0).
+// delta is formed from P and dP, in a first walk over the keys. It equals sum_c dO_ic O_ic, which costs no walk, but O comes
+// rounded to 16 bits, and an error of delta does not average out: dS of a row is off by P times it. Measured on 12 heads of
+// 32760 rows and 512 keys in bf16, rms errors of dQ / dK relative to their size, and the time of the gradients: from O 0.0038 /
+// 0.0030, 405 us; from P and dP 0.0024 / 0.0024 (a rounding of dQ itself: 0.0017). With one key, dS is exactly 0.
 #include <type_traits>
 
 #include "cross_common.hpp"
@@ -35,24 +36,6 @@ constexpr int RT = 32;         // rows of its tiles
 __host__ __device__ __forceinline__ int stat_rows(int M) { return (M + RT - 1) / RT * RT; }
 
 template <int DT>
-__device__ __forceinline__ float dot8(u4 a, u4 b, float s) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t x = a[i], y = b[i];
-    if constexpr (DT == VC_BF16) {
-      s = __builtin_fmaf(bf16_lo(x), bf16_lo(y), s);
-      s = __builtin_fmaf(bf16_hi(x), bf16_hi(y), s);
-    } else {
-      typedef _Float16 h2 __attribute__((ext_vector_type(2)));
-      const h2 u = __builtin_bit_cast(h2, x), v = __builtin_bit_cast(h2, y);
-      s = __builtin_fmaf((float)u[0], (float)v[0], s);
-      s = __builtin_fmaf((float)u[1], (float)v[1], s);
-    }
-  }
-  return s;
-}
-
-template <int DT>
 __device__ __forceinline__ u4 pack_half(const v16f& s, int h) {
   u4 r;
 #pragma unroll
@@ -60,8 +43,12 @@ __device__ __forceinline__ u4 pack_half(const v16f& s, int h) {
   return r;
 }
 
-// GATHER: addresses per key (the keys are those of a list, or their stride is too far for one buffer); SPLIT: leave parts
-template <int DT, int D, bool GATHER, bool SPLIT>
+// What a launch of cross_dq forms: delta and dQ in two walks over all keys; or over a part of the keys its part of delta, and in
+// a second launch its part of dQ
+enum { WHOLE, PART_DELTA, PART_DQ };
+
+// GATHER: addresses per key (the keys are those of a list, or their stride is too far for one buffer)
+template <int DT, int D, bool GATHER, int MODE>
 __global__ __launch_bounds__(64 * NW, 2) void cross_dq(CrossArgs a) {
   using T = Tile<D>;
   using C = Copier<D, KT, NW>;
@@ -76,33 +63,35 @@ __global__ __launch_bounds__(64 * NW, 2) void cross_dq(CrossArgs a) {
   const int lane = threadIdx.x & 63, col = lane & 31, kh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = keys_of(a, b);
-  const int k0 = SPLIT ? split * a.chunk : 0, k1 = SPLIT ? min(n, k0 + a.chunk) : n;
+  const int k0 = MODE == WHOLE ? 0 : split * a.chunk, k1 = MODE == WHOLE ? n : min(n, k0 + a.chunk);
   const int tiles = k1 > k0 ? (k1 - k0 + KT - 1) / KT : 0;
+  const int steps = MODE == WHOLE ? 2 * tiles : tiles;   // tiles in the order of both walks
 
   const uint16_t *kbase = a.K.p + b * a.K.sb + hk * a.K.sh, *vbase = a.V.p + b * a.V.sb + hk * a.V.sh;
   const int crow = lane / T::CH;
   const C kc(a.K.sn, wave, lane), vc(a.V.sn, wave, lane);
   int next[C::COPIES];
-  auto fetch = [&](int t) __attribute__((always_inline)) {
+  auto fetch = [&](int u) __attribute__((always_inline)) {
     if (GATHER) {
+      const int t = u < tiles ? u : u - tiles;
 #pragma unroll
-      for (int u = 0; u < C::COPIES; ++u) {
-        const int j = k0 + t * KT + (u * NW + wave) * T::ROWS_PER_COPY + crow;
-        next[u] = j < k1 ? (a.idx ? a.idx[(size_t)b * a.N + j] : j) : -1;
+      for (int c = 0; c < C::COPIES; ++c) {
+        const int j = k0 + t * KT + (c * NW + wave) * T::ROWS_PER_COPY + crow;
+        next[c] = u < steps && j < k1 ? (a.idx ? a.idx[(size_t)b * a.N + j] : j) : -1;
       }
     }
   };
-  auto copy_tile = [&](int t, int buf) __attribute__((always_inline)) {
+  auto copy_tile = [&](int u, int buf) __attribute__((always_inline)) {
     if (GATHER) {
 #pragma unroll
-      for (int u = 0; u < C::COPIES; ++u) {
-        const int q = u * NW + wave, ch = (lane % T::CH) ^ T::key(q * T::ROWS_PER_COPY + crow);
-        const int64_t src = next[u];
+      for (int c = 0; c < C::COPIES; ++c) {
+        const int q = c * NW + wave, ch = (lane % T::CH) ^ T::key(q * T::ROWS_PER_COPY + crow);
+        const int64_t src = next[c];
         copy16(src >= 0 ? (const void*)(kbase + src * a.K.sn + 8 * ch) : (const void*)&zero16, kt[buf] + q * 1024);
         copy16(src >= 0 ? (const void*)(vbase + src * a.V.sn + 8 * ch) : (const void*)&zero16, vt[buf] + q * 1024);
       }
     } else {
-      const int j = k0 + t * KT;
+      const int j = k0 + (u < tiles ? u : u - tiles) * KT;
       kc.copy(kbase + j * a.K.sn, k1 - j, kt[buf], wave);
       vc.copy(vbase + j * a.V.sn, k1 - j, vt[buf], wave);
     }
@@ -117,20 +106,20 @@ __global__ __launch_bounds__(64 * NW, 2) void cross_dq(CrossArgs a) {
   const bool active = r0 < a.R;
   const QueryRow qr = query_row(a, hk, min(row, a.R - 1));
   u4 q[KS], g[KS];
-  float delta = 0.f;
   {
     const uint16_t* pq = a.Q.p + b * a.Q.sb + qr.h * a.Q.sh + qr.i * a.Q.sn + 8 * kh;
     const uint16_t* pg = a.dO.p + b * a.dO.sb + qr.h * a.dO.sh + qr.i * a.dO.sn + 8 * kh;
-    const uint16_t* po = a.O.p + b * a.O.sb + qr.h * a.O.sh + qr.i * a.O.sn + 8 * kh;
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
       q[s] = *reinterpret_cast<const u4*>(pq + 16 * s);
       g[s] = *reinterpret_cast<const u4*>(pg + 16 * s);
-      delta = dot8<DT>(g[s], *reinterpret_cast<const u4*>(po + 16 * s), delta);
     }
   }
-  delta = half_sum(delta);
   const float l2 = a.lse[((size_t)b * a.Hq + qr.h) * a.M + qr.i] * 1.4426950408889634f;
+  const size_t heads = (size_t)a.B * a.Hk;
+  float delta = 0.f;   // in the first walk, the sum of this lane's keys
+  if (MODE == PART_DQ && row < a.R)
+    for (int s = 0; s < a.splits; ++s) delta += a.part_ml[(s * heads + bh) * a.R + row];
   const RowOperands<D> rows0(lane);
   const ColOperands<D> cols0(lane);
   v16f acc[DB];
@@ -155,43 +144,57 @@ __global__ __launch_bounds__(64 * NW, 2) void cross_dq(CrossArgs a) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], a.c, -l2));
   };
-  for (int t = 0; t < tiles; ++t) {
+  // tile u (of both walks) is there, the next on its way
+  auto arrive = [&](int u) __attribute__((always_inline)) {
     wait_copies<0>();
     barrier();
-    if (t + 1 < tiles) {
-      copy_tile(t + 1, (t + 1) & 1);
-      fetch(t + 2);
+    if (u + 1 < steps) {
+      copy_tile(u + 1, (u + 1) & 1);
+      fetch(u + 2);
     }
-    if (!active) continue;
-    const int valid = k1 - k0 - t * KT;
-    v16f s, dp;
-    if (n <= KT) {
-      float d = 0.f;
-#pragma unroll 1
+  };
+  int u = 0;
+  if (MODE != PART_DQ) {
+    for (; u < tiles; ++u) {
+      arrive(u);
+      if (!active) continue;
+#pragma unroll
       for (int x = 0; x < 2; ++x) {
-        products(0, x, valid, s, dp);
+        v16f s, dp;
+        products((u & 1) * TB, x, k1 - k0 - u * KT, s, dp);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) d = __builtin_fmaf(s[r], dp[r], d);
+        for (int r = 0; r < 16; ++r) delta = __builtin_fmaf(s[r], dp[r], delta);
       }
-      delta = half_sum(d);
     }
+    delta = half_sum(delta);
+  }
+  if (MODE != PART_DELTA) {
+    for (int t = 0; t < tiles; ++t, ++u) {
+      arrive(u);
+      if (!active) continue;
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      products((t & 1) * TB, x, valid, s, dp);
+      for (int x = 0; x < 2; ++x) {
+        v16f s, dp;
+        products((u & 1) * TB, x, k1 - k0 - t * KT, s, dp);
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] *= dp[r] - delta;
-      const u4 ds[2] = {pack_half<DT>(s, 0), pack_half<DT>(s, 1)};
-      __builtin_amdgcn_sched_barrier(0);
-      const ColOperands<D> cols = cols0.move(lds_addr(kt[0]) + (t & 1) * TB);
+        for (int r = 0; r < 16; ++r) s[r] *= dp[r] - delta;
+        const u4 ds[2] = {pack_half<DT>(s, 0), pack_half<DT>(s, 1)};
+        __builtin_amdgcn_sched_barrier(0);
+        const ColOperands<D> cols = cols0.move(lds_addr(kt[0]) + (u & 1) * TB);
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int db = 0; db < DB; ++db) acc[db] = mma<DT>(cols.get((32 * x + 16 * h) * T::ROW, db), ds[h], acc[db]);
-      issue_reads<8>();
-      issue_products<2 * DB - 4, 2>();
-      issue_products<4, 0>();
-      __builtin_amdgcn_sched_barrier(0);
+          for (int db = 0; db < DB; ++db) acc[db] = mma<DT>(cols.get((32 * x + 16 * h) * T::ROW, db), ds[h], acc[db]);
+        issue_reads<8>();
+        issue_products<2 * DB - 4, 2>();
+        issue_products<4, 0>();
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
+  }
+  if (MODE == PART_DELTA) {
+    if (row < a.R && kh == 0) a.part_ml[(split * heads + bh) * a.R + row] = delta;
+    return;
   }
 
   // what cross_dkv needs of a row; the rows that fill a head's last tile get probabilities of 0
@@ -202,9 +205,9 @@ __global__ __launch_bounds__(64 * NW, 2) void cross_dq(CrossArgs a) {
     if (qr.i == a.M - 1)
       for (int i = 1; i < fill - qr.i; ++i) *reinterpret_cast<float2*>(st + 2 * i) = make_float2(INFINITY, 0.f);
   }
-  if (SPLIT) {
+  if (MODE == PART_DQ) {
     if (row < a.R) {
-      float* p = a.part_o + (((size_t)split * a.B * a.Hk + bh) * a.R + row) * D + 4 * kh;
+      float* p = a.part_o + ((split * heads + bh) * a.R + row) * D + 4 * kh;
 #pragma unroll
       for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -441,13 +444,16 @@ hipError_t backward(const CrossArgs& a, hipStream_t s) {
   const bool far = a.Q.sn >= FAR_STRIDE || a.dO.sn >= FAR_STRIDE;
   hipError_t e;
   if (a.splits > 1) {
-    if (gather) cross_dq<DT, D, true, true><<<gq, 64 * NW, 0, s>>>(a);
-    else cross_dq<DT, D, false, true><<<gq, 64 * NW, 0, s>>>(a);
+    if (gather) cross_dq<DT, D, true, PART_DELTA><<<gq, 64 * NW, 0, s>>>(a);
+    else cross_dq<DT, D, false, PART_DELTA><<<gq, 64 * NW, 0, s>>>(a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    if (gather) cross_dq<DT, D, true, PART_DQ><<<gq, 64 * NW, 0, s>>>(a);
+    else cross_dq<DT, D, false, PART_DQ><<<gq, 64 * NW, 0, s>>>(a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     cross_join_dq<DT, D><<<(unsigned)((heads * a.R + jq - 1) / jq), 256, 0, s>>>(a, gj);
   } else {
-    if (gather) cross_dq<DT, D, true, false><<<gq, 64 * NW, 0, s>>>(a);
-    else cross_dq<DT, D, false, false><<<gq, 64 * NW, 0, s>>>(a);
+    if (gather) cross_dq<DT, D, true, WHOLE><<<gq, 64 * NW, 0, s>>>(a);
+    else cross_dq<DT, D, false, WHOLE><<<gq, 64 * NW, 0, s>>>(a);
   }
   if ((e = hipGetLastError()) != hipSuccess) return e;
   if (a.row_splits > 1) {

@@ -75,8 +75,7 @@ def norm_rope_grad(x, w, cos, sin, layout, rot, norm, eps, dz):
 class Cross:
     """Attention to another sequence and its gradients in 64 bits, with bounds of a kernel's errors.
 
-    What a kernel may do: round P and dS to the type (half a step each), round outputs (half a step), use the rounded O
-    in delta where a row has more than 64 keys, and compute in fp32: scores of d products (d + 8 steps of 2^-24 of the
+    What a kernel may do: round P and dS to the type (half a step each), round outputs (half a step), and compute in fp32: scores of d products (d + 8 steps of 2^-24 of the
     sum of their sizes, in log2 units, which the exponential turns into a relative error, once for the score and once
     for lse), sums over the keys (at most N + 64 additions of 2^-24 each). In fp16 P and dS below the normal range
     round absolutely (TINY).
@@ -112,9 +111,7 @@ class Cross:
         dPs = G.abs() @ Vg.abs().transpose(2, 3)
         delta = (P * dP).sum(3, keepdim=True)
         dS = P * (dP - delta)
-        few = (valid.sum(1) <= 64).view(B, 1, 1, 1)
-        derr = torch.where(few, ((rel + d * 2.0 ** -24) * P * dPs).sum(3, keepdim=True),
-                           (G.abs() * (self.O_err + d * 2.0 ** -24 * A)).sum(3, keepdim=True))
+        derr = ((rel + d * 2.0 ** -24) * P * dPs).sum(3, keepdim=True)
         dSerr = P * ((half + rel) * (dP - delta).abs() + d * 2.0 ** -24 * dPs + derr) * (1 + half)
         Pt = P.transpose(2, 3)
         self.dV, self.dQ = group(Pt @ G), dS @ Kg * scale
