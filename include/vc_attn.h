@@ -386,7 +386,8 @@ vc_status vc_rope_line_tables(int32_t rows, int32_t rot, double theta, const vc_
 
 /* Shape of the attention to another sequence: B items, Hq query heads of M queries, Hk key heads of N keys, d = 64 or
  * 128 channels; query head h attends to key head h / (Hq / Hk). All sizes >= 1, Hq a multiple of Hk,
- * B * Hq * M < 2^31, B * Hk * N < 2^31 and (Hq / Hk) * M, N <= 2^30 (VC_ERR_SHAPE otherwise). */
+ * B * Hq * M < 2^31, B * Hk * N < 2^31, (Hq / Hk) * M and N <= 2^30, and B * Hk * ceil(x / 128) < 2^24 for
+ * x = (Hq / Hk) * M and x = N (VC_ERR_SHAPE otherwise). */
 typedef struct {
     int32_t B, Hq, Hk, M, N, d;
 } vc_cross_shape;
@@ -430,7 +431,9 @@ vc_status vc_cross_attn_forward(const vc_cross_shape *shape, const vc_cross_opts
                                 void *stream);
 
 /* Gradients of vc_cross_attn_forward.
- *   Q, K, V, k_len, k_mask, O, lse : as given to and written by vc_cross_attn_forward.
+ *   Q, K, V, k_len, k_mask, lse : as given to and written by vc_cross_attn_forward.
+ *   O          : as written by vc_cross_attn_forward, or NULL. It is checked but not read: the rows' sums of P dP are
+ *                formed from the operands, since O comes rounded to 16 bits.
  *   dO         : gradient of O, [B, Hq, M, d].
  *   dQ, dK, dV : gradients, written (not added to), shapes of Q, K, V; they must not overlap an input or each other.
  *                dK and dV are summed over the query heads of their key head; where K or V is shared along an axis by a

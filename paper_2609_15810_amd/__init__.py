@@ -513,7 +513,7 @@ class CrossAttention(_Operator):
         self._call("vc_cross_attn_forward", stream, *self._inputs(Q, K, V, k_len, k_mask, O, lse), *self._ws)
 
     def backward(self, Q, K, V, O, lse, dO, dQ, dK, dV, k_len=None, k_mask=None, stream=None):
-        """dQ, dK, dV from dO, with O and lse as forward() wrote them (training=True)."""
+        """dQ, dK, dV from dO, with O (or None: it is not read) and lse as forward() wrote them (training=True)."""
         self._call("vc_cross_attn_backward", stream, *self._inputs(Q, K, V, k_len, k_mask, O, lse),
                    self._view(dO, self._q), self._view(dQ, self._q), self._view(dK, self._k), self._view(dV, self._k),
                    *self._ws)

@@ -104,7 +104,10 @@ vc_status check_cross(const vc_cross_shape* s, const vc_cross_opts* o) {
   const int64_t top = 1LL << 31;
   if ((int64_t)s->B * s->Hq >= top || (int64_t)s->B * s->Hq * s->M >= top || (int64_t)s->B * s->Hk * s->N >= top)
     return VC_ERR_SHAPE;
-  if ((int64_t)(s->Hq / s->Hk) * s->M > (1 << 30) || s->N > (1 << 30)) return VC_ERR_SHAPE;
+  const int64_t rows = (int64_t)(s->Hq / s->Hk) * s->M, heads = (int64_t)s->B * s->Hk;
+  if (rows > (1 << 30) || s->N > (1 << 30)) return VC_ERR_SHAPE;
+  // workgroups of 128 rows or keys: a launch has fewer than 2^32 threads
+  if ((rows + 127) / 128 * heads >= (1 << 24) || ((int64_t)s->N + 127) / 128 * heads >= (1 << 24)) return VC_ERR_SHAPE;
   if (o->dtype != VC_BF16 && o->dtype != VC_FP16) return VC_ERR_UNSUPPORTED;
   if (!(o->sm_scale >= 0.f) || !std::isfinite(o->sm_scale * 1.4426950408889634f)) return VC_ERR_UNSUPPORTED;
   if (o->masked != 0 && o->masked != 1) return VC_ERR_UNSUPPORTED;
@@ -220,7 +223,7 @@ vc_status vc_cross_attn_backward(const vc_cross_shape* shape, const vc_cross_opt
   vc_status st = cross_inputs(shape, opts, Q, K, V, k_len, k_mask, k_mask_stride, ws, ws_bytes, true, a);
   if (st != VC_OK) return st;
   const int B = shape->B, Hq = shape->Hq, Hk = shape->Hk, M = shape->M, N = shape->N, d = shape->d;
-  if ((st = cross_view(O, B, Hq, M, d, false, a.O)) != VC_OK) return st;
+  if (O && (st = cross_view(O, B, Hq, M, d, false, a.O)) != VC_OK) return st;
   if ((st = cross_view(dO, B, Hq, M, d, false, a.dO)) != VC_OK) return st;
   if ((st = cross_view(dQ, B, Hq, M, d, true, a.dQ)) != VC_OK) return st;
   if ((st = cross_view(dK, B, Hk, N, d, true, a.dK)) != VC_OK) return st;

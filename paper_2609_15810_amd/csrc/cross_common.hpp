@@ -141,13 +141,6 @@ __device__ __forceinline__ void copy16(const void* src, const void* lds) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "s"(to) : "memory", "m0");
 }
 
-// Bring the line at p near: 4 bytes a lane into 256 bytes of LDS that nobody reads. (A load into a register would be waited
-// for where the register is next touched, and the tile copies behind it with it.)
-__device__ __forceinline__ void touch(const void* p, const void* lds) {
-  const uint32_t to = __builtin_amdgcn_readfirstlane(lds_addr(lds));
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(p), "s"(to) : "memory", "m0");
-}
-
 // Scores of the keys (rows of a 32x32 result) behind the first `valid` become -inf. For a branch that is taken once a row
 // block at most; the pin keeps the comparisons in it.
 __device__ __forceinline__ void mask_scores(v16f& s, int valid, int kh) {

@@ -10,7 +10,14 @@
 // tile ahead.
 //
 // The rows of a key head are those of all its query heads, one head behind the other, so that grouped heads share
-// tiles and a token's few queries share one.
+// tiles and a token's few queries share one. Calls with rows for 256 workgroups of 256 take cross_fwd_wide instead, whose
+// workgroups walk over blocks of rows of a head. Measured (us, this kernel / wide): 12 heads of 32760 rows over 512 keys 129 /
+// 122, over 1024 keys 232 / 214; 40 heads of 75600 rows over 512 keys 1099 / 1036 (1.5 GB, 793 GFLOP); with 192 workgroups
+// (12 heads of 4096 rows) 26 / 26, below that it loses CUs.
+//
+// What bounds it: 16 bytes of LDS are read per product and lane, exponentials and products take about the same time, and the
+// card lowers its clock under the matrix cores' load (1.7 GHz at their full rate on random operands); the sustained rate of
+// a large library product here is 1.06 to 1.35 PFLOP/s, of this kernel 0.85.
 //
 // Few rows and long keys: the keys are split over workgroups (cross_plan), each leaves unnormalised fp32 outputs with its
 // maximum and sum, and cross_join adds them up in a fixed order.
@@ -311,13 +318,13 @@ __global__ __launch_bounds__(64 * WW, 2) void cross_fwd_wide(CrossArgs a, int to
 #pragma unroll
         for (int db = 0; db < DB; ++db) o[db] = mma<DT>(cols.get(16 * i * T::ROW, db), p[i], o[db]);
     };
-    auto probabilities = [&](int valid) __attribute__((always_inline)) {
+    auto probabilities = [&](bool first, int valid) __attribute__((always_inline)) {
       if (valid < KT) mask_scores(s, valid, kh);
       float top = fmaxf(s[0][0], s[1][0]);
 #pragma unroll
       for (int r = 1; r < 16; ++r) top = fmaxf(fmaxf(top, s[0][r]), s[1][r]);
       top = half_max(top) * a.c;
-      if (__builtin_amdgcn_ballot_w64(top > m + LAG)) {
+      if (first || __builtin_amdgcn_ballot_w64(top > m + LAG)) {   // (the first tile of a block always clears its sums)
         const float up = top > m + LAG ? top : m, alpha = __builtin_amdgcn_exp2f(m - (up == -INFINITY ? 0.f : up));
         const bool anew = m == -INFINITY;   // (selected, not multiplied: what stands there may not be finite)
         m = up;
@@ -356,7 +363,7 @@ __global__ __launch_bounds__(64 * WW, 2) void cross_fwd_wide(CrossArgs a, int to
       copy_pair();
       if (stored) finish(x - 1);   // the block before the one at work is complete
       const bool last = t + 1 == tiles;
-      probabilities(n - t * KT);
+      probabilities(t == 0, n - t * KT);
       if (last && x + 1 < count) {
         load_queries();
         if (x + 2 < count) copy_queries(x + 2);

@@ -51,7 +51,8 @@ BAD = vc.View(None, 0, 0, 0)
 
 @pytest.mark.parametrize("kw", [dict(B=0), dict(Hq=0), dict(Hk=0), dict(M=0), dict(N=0), dict(d=96), dict(d=32),
                                 dict(Hq=3), dict(B=1 << 20, M=1 << 10), dict(B=1 << 20, N=1 << 10),
-                                dict(Hk=1, B=1, M=(1 << 28) + 1), dict(Hq=1, Hk=1, B=1, N=(1 << 30) + 1)])
+                                dict(Hk=1, B=1, M=(1 << 28) + 1), dict(Hq=1, Hk=1, B=1, N=(1 << 30) + 1),
+                                dict(B=1 << 23, M=1, N=1)])
 def test_shapes_refused(L, kw):
     s = shape(**kw)
     assert forward(L, s, opts()) == 2 and backward(L, s, opts()) == 2
@@ -81,6 +82,8 @@ def test_views_refused(L, name):
 def test_backward_views_refused(L, name):
     s, o = shape(), opts()
     H, n = (2, 30) if name in ("dK", "dV") else (4, 50)
+    if name != "O":
+        assert backward(L, s, o, **{name: None}) == 1
     assert backward(L, s, o, **{name: BAD}) == 1
     assert backward(L, s, o, **{name: view(H, n, data=FAKE + 8)}) == 5
     if name[0] == "d" and name != "dO":   # outputs whose rows overlap

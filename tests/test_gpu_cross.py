@@ -235,6 +235,25 @@ def test_values_that_are_not_finite():
     assert torch.equal(out[:, :, rows], clean[:, :, rows])
 
 
+@pytest.mark.parametrize("B,H,M,N", [(1, 2, 40, 200), (4, 40, 300, 200), (1, 2, 3, 4000)])
+def test_scores_of_minus_infinity(B, H, M, N):
+    # keys whose scores are -inf take no part; a row all of whose scores are -inf has no softmax (NaN), and the rows
+    # that the same waves work on next are not touched by it
+    p = Problem(B, H, H, M, N)
+    p.Q.abs_()
+    p.cpu[0] = p.cpu[0].abs()
+    p.K[:, :, :70, 0] = -float("inf")
+    p.valid[:, :70] = False
+    out, lse = p.forward()
+    q, k, v, _ = p.cpu
+    ref = O.Cross(q, k, v, p.valid, BF)
+    near(out, ref.O, ref.O_err, "O")
+    p.K[0, 0, :, 0] = -float("inf")
+    out, lse = p.forward()
+    assert out[0, 0].isnan().all()
+    near(out[:, 1:], ref.O[:, 1:], ref.O_err[:, 1:], "O")
+
+
 def test_gradient_against_differences():
     """sum(O dO) along directions of Q, K and V by central differences of the forward kernel in fp16: each value of O is
     off by half a step and P's rounding, and the step's third-order part is the cube of its size."""
