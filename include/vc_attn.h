@@ -318,11 +318,12 @@ typedef struct {
  *   layout : as above. With VC_ROPE_NONE, norm must not be VC_NORM_NONE.
  *   rot    : channels that are turned, the first `rot` of each head: a multiple of 16, 16 <= rot <= d (0 with
  *            VC_ROPE_NONE). The others pass (normed) as they are.
- *   eps    : > 0 and finite where there is a norm.
+ *   eps    : a normal positive fp32 number (>= 2^-126, finite) where there is a norm.
  *   rows   : rows of the tables for positions on a line (F = 0): [rows, rot/2] fp32, row p the cos / sin of
  *            position p (vc_rope_line_tables). rows >= 1.
  *   F, Ht, Wd : all 0 (a line), or a latent grid with F * Ht * Wd = N: token n turns by its frame, row and column with
- *            the tables of vc_rope_tables ([F + Ht + Wd, 64]); d and rot must then be 128. `rows` is not used.
+ *            the tables of vc_rope_tables ([F + Ht + Wd, 64], F + Ht + Wd < 2^25: VC_ERR_SHAPE); d and rot must then be
+ *            128. `rows` is not used.
  * VC_ERR_UNSUPPORTED for a value outside these. */
 typedef struct {
     int32_t dtype, norm, layout, rot;

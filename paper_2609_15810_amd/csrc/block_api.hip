@@ -1,5 +1,6 @@
 // C ABI of the operators around the attention (declared in include/vc_attn.h): argument validation on the
 // host, workspace carve-up and launches of the norms with the rotation and of the attention to another sequence.
+#include <cfloat>
 #include <cmath>
 #include <cstdint>
 
@@ -53,7 +54,7 @@ vc_status check_norm_rope(const vc_norm_rope_shape* s, const vc_norm_rope_opts* 
   if (o->layout != VC_ROPE_NONE && o->layout != VC_ROPE_INTERLEAVED && o->layout != VC_ROPE_HALF)
     return VC_ERR_UNSUPPORTED;
   if (o->norm == VC_NORM_NONE && o->layout == VC_ROPE_NONE) return VC_ERR_UNSUPPORTED;
-  if (o->norm != VC_NORM_NONE && !(o->eps > 0.f && std::isfinite(o->eps))) return VC_ERR_UNSUPPORTED;
+  if (o->norm != VC_NORM_NONE && !(o->eps >= FLT_MIN && std::isfinite(o->eps))) return VC_ERR_UNSUPPORTED;
   if (o->norm == VC_NORM_TOKEN && (s->Hq * s->d > 8192 || s->Hk * s->d > 8192)) return VC_ERR_SHAPE;
   if (o->layout == VC_ROPE_NONE) return o->rot == 0 ? VC_OK : VC_ERR_UNSUPPORTED;
   if (o->rot < 16 || o->rot > s->d || o->rot % 16 != 0) return VC_ERR_UNSUPPORTED;
@@ -61,6 +62,7 @@ vc_status check_norm_rope(const vc_norm_rope_shape* s, const vc_norm_rope_opts* 
   if (o->F < 1 || o->Ht < 1 || o->Wd < 1) return VC_ERR_UNSUPPORTED;
   const int64_t fh = (int64_t)o->F * o->Ht;
   if (fh > s->N || fh * o->Wd != s->N) return VC_ERR_SHAPE;
+  if ((int64_t)o->F + o->Ht + o->Wd >= (1 << 25)) return VC_ERR_SHAPE;   // the kernels' indexes into the tables
   if (s->d != 128 || o->rot != 128) return VC_ERR_UNSUPPORTED;
   return VC_OK;
 }

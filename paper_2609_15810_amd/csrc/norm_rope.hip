@@ -4,7 +4,7 @@
 // H d channels of the token) and weights w,
 //   r = 1 / sqrt(mean_S(x^2) + eps),  y = x r w,  z = R(pos) y,
 // where R turns the pairs of the first `rot` channels by the token's angles. With g = R^T dz,
-//   dw = sum over rows of g x r,  dx = r (g w - x r^2 mean_S(g w x)).
+//   dw = sum over rows of g u,  dx = r (g w - u mean_S(g w u)),  u = x r.
 // R^T is R with the sines negated (also where the tables carry a factor), so the gradient of the rotation
 // alone is the forward kernel with that sign.
 //
@@ -146,16 +146,19 @@ __device__ __forceinline__ void load_angles(const NormRopeArgs& a, const Lane& l
   for (int i = 0; i < 8; ++i) sn[i] *= sign;
 }
 
-// turn the pairs of x (16 channels: piece 0, then piece 1)
+// turn the pairs of x (16 channels: piece 0, then piece 1); the channels that are not turned stay as they are (a product with
+// a sine of 0 would carry an infinity or NaN from one into another)
 template <int LAYOUT>
-__device__ __forceinline__ void turn(float* x, const float* cs, const float* sn) {
+__device__ __forceinline__ void turn(float* x, const Lane& l, const float* cs, const float* sn) {
   if (LAYOUT == VC_ROPE_NONE) return;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int ia = LAYOUT == VC_ROPE_HALF ? i : 2 * i, ib = LAYOUT == VC_ROPE_HALF ? i + 8 : 2 * i + 1;
+    const bool on = i < 4 ? l.turn0 : l.turn1;
     const float u = x[ia], v = x[ib];
-    x[ia] = __builtin_fmaf(u, cs[i], -v * sn[i]);
-    x[ib] = __builtin_fmaf(u, sn[i], v * cs[i]);
+    const float s = __builtin_fmaf(u, cs[i], -v * sn[i]), t = __builtin_fmaf(u, sn[i], v * cs[i]);
+    x[ia] = on ? s : u;
+    x[ib] = on ? t : v;
   }
 }
 
@@ -311,7 +314,7 @@ __global__ __launch_bounds__(64 * WAVES, 3) void norm_rope_fwd(NormRopeArgs a) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) v[e] = v[e] * r * wt[NORM == VC_NORM_TOKEN ? i : 0][e];
       }
-      turn<LAYOUT>(v, cs, sn);
+      turn<LAYOUT>(v, l, cs, sn);
       if (p.live && h < x.H) {
         store_row(out + h * x.out_sh, l, pack8<DT>(v), pack8<DT>(v + 8), a.past);
       }
@@ -396,7 +399,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void norm_rope_bwd(NormRopeArgs a) {
         unpack8<DT>(raw[i][1], v + 8);
         unpack8<DT>(gr[i][0], g);
         unpack8<DT>(gr[i][1], g + 8);
-        turn<LAYOUT>(g, cs, sn);
+        turn<LAYOUT>(g, l, cs, sn);
       };
       float t[2] = {0.f, 0.f};   // sums of x^2 and of g w x
       auto add = [&](int i, const float* v, const float* g) __attribute__((always_inline)) {
@@ -429,11 +432,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void norm_rope_bwd(NormRopeArgs a) {
           t[1] = lanes_sum(t[1], G);
         }
         const float r = __builtin_amdgcn_rsqf(__builtin_fmaf(t[0], x.inv_span, a.eps));
-        const float k = r * r * r * (t[1] * x.inv_span);   // r^3 mean(g w x)
+        const float k = t[1] * x.inv_span * r;   // mean(g w u) with u = x r: of the size of g w, whatever r is
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          dw[iw][e] = __builtin_fmaf(g[e] * r, v[e], dw[iw][e]);
-          g[e] = __builtin_fmaf(-k, v[e], g[e] * wt[iw][e] * r);
+          const float u = v[e] * r;
+          dw[iw][e] = __builtin_fmaf(g[e], u, dw[iw][e]);
+          g[e] = __builtin_fmaf(-k, u, g[e] * wt[iw][e]) * r;
         }
         if (u.p.live && h < x.H) {
           store_row(out + h * x.out_sh, l, pack8<DT>(g), pack8<DT>(g + 8), a.past);

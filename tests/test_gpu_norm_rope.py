@@ -263,3 +263,32 @@ def test_streams_and_graph():
         other.backward()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out + [dq, dk] + dw, ref + rg + rw))
+
+
+@pytest.mark.parametrize("layout,rot", [("half", 32), ("half", 112), ("interleaved", 48)])
+def test_channels_behind_the_turned_part_stay_as_they_are(layout, rot):
+    p = Problem(1, 3, 2, 21, 128, FP, "none", layout, rot)
+    p.q[0, 0, 4, rot + 1], p.q[0, 1, 5, 127], p.k[0, 0, 6, rot] = float("inf"), float("nan"), -0.0
+    p.q[0, 2, 9, rot + 3] = -0.0
+    bits = lambda t: t[..., rot:].contiguous().view(torch.int16)  # noqa: E731
+    for x, z in zip((p.q, p.k), p.forward()):
+        assert torch.equal(bits(x), bits(z))
+        assert z[..., :rot].isfinite().all()
+
+
+@pytest.mark.parametrize("norm", ["head", "token"])
+@pytest.mark.parametrize("eps", [1e-30, 2.0 ** -126])
+def test_small_eps(norm, eps):
+    """1 / sqrt(eps) whose cube is beyond fp32: rows of zeros and ordinary ones (as check(), with this eps)"""
+    p = Problem(1, 2, 1, 12, 128, BF, norm, "none", 0)
+    p.q[:, :, 3] = 0.0
+    p.op = vc.NormRope(1, 2, 1, 12, norm=NORMS[norm], eps=eps, layout=vc.ROPE_NONE, training=True)
+    out, (grads, dw) = p.forward(), p.backward()
+    eps = float(torch.tensor(eps))
+    x, w, dz = p.q.cpu().double(), p.w[0].double(), p.dz[0].double()
+    ref = O.norm_rope(x, w, p.c, p.s, "none", 0, norm, eps)
+    assert ((out[0].cpu().double() - ref).abs() <= (2.0 ** -8 + 2.0 ** -16) * ref.abs() + 2.0 ** -134).all()
+    dx, dwr, dxs, dws = O.norm_rope_grad(x, w, p.c, p.s, "none", 0, norm, eps, dz)
+    err = (grads[0].cpu().double() - dx).abs()
+    assert (err <= 2.0 ** -8 * (dx.abs() + 2.0 ** -15 * dxs) + 2.0 ** -15 * dxs + 2.0 ** -134).all()
+    assert ((dw[0].cpu().double() - dwr).abs() <= 2.0 ** -14 * dws).all()

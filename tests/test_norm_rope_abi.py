@@ -54,7 +54,7 @@ def test_shapes_refused(L, kw):
 
 
 @pytest.mark.parametrize("kw", [dict(dtype=2), dict(norm=3), dict(norm=-1), dict(layout=3), dict(rot=0), dict(rot=24),
-                                dict(rot=144), dict(eps=0.0), dict(eps=math.nan), dict(eps=math.inf), dict(rows=0),
+                                dict(rot=144), dict(eps=0.0), dict(eps=1e-39), dict(eps=math.nan), dict(eps=math.inf), dict(rows=0),
                                 dict(grid=(4, 0, 0)), dict(norm=vc.NORM_NONE, layout=vc.ROPE_NONE, rot=0),
                                 dict(layout=vc.ROPE_NONE)])
 def test_options_refused(L, kw):
@@ -65,6 +65,8 @@ def test_other_refusals(L):
     s, o = shape(), opts()
     assert forward(L, shape(Hq=65), opts(norm=vc.NORM_TOKEN)) == 2            # more than 8192 channels under one norm
     assert forward(L, s, opts(grid=(3, 4, 6))) == 2                           # 72 tokens, not 60
+    far = shape(B=1, N=1 << 25)                                               # rows of the tables beyond 32-bit indexes
+    assert forward(L, far, opts(grid=(1 << 25, 1, 1))) == 2
     assert forward(L, shape(d=64), opts(rot=64, grid=(3, 4, 5))) == 3         # the grid's tables are for 128 channels
     assert forward(L, s, opts(grid=(3, 4, 5)), pos=FAKE) == 3
     assert forward(L, s, opts(rows=59)) == 2                                  # fewer rows than tokens
