@@ -387,7 +387,7 @@ vc_status vc_rope_line_tables(int32_t rows, int32_t rot, double theta, const vc_
 
 /* Shape of the attention to another sequence: B items, Hq query heads of M queries, Hk key heads of N keys, d = 64 or
  * 128 channels; query head h attends to key head h / (Hq / Hk). All sizes >= 1, Hq a multiple of Hk,
- * B * Hq * M < 2^31, B * Hk * N < 2^31, (Hq / Hk) * M and N <= 2^30, and B * Hk * ceil(x / 128) < 2^24 for
+ * B * Hq * M < 2^31, B * Hk * N < 2^31, (Hq / Hk) * M and N <= 2^30, B < 2^22, and B * Hk * ceil(x / 128) < 2^24 for
  * x = (Hq / Hk) * M and x = N (VC_ERR_SHAPE otherwise). */
 typedef struct {
     int32_t B, Hq, Hk, M, N, d;
@@ -396,8 +396,9 @@ typedef struct {
 /* Options of the attention to another sequence.
  *   dtype    : VC_BF16 or VC_FP16, of all tensors. The products take 16-bit operands: the probabilities (and in the
  *              backward pass their gradients) are rounded to dtype before they enter a product. Sums and the softmax's
- *              statistics are fp32, outputs are rounded once. With VC_FP16, gradients of scores (dS, of the size of
- *              dO times V) have fp16's range: a loss scaled as for any fp16 training keeps them there.
+ *              statistics are fp32, outputs are rounded once. With VC_FP16, probabilities of the backward pass and
+ *              gradients of scores (dS, of the size of dO times V) have fp16's range: in steps of 2^-24 at the
+ *              least, and dS below 65520, where a loss scaled as for any fp16 training keeps it.
  *   sm_scale : score scale, >= 0 with sm_scale * log2(e) finite in fp32; 0 selects 1/sqrt(d).
  *   masked   : 1 = the calls give a k_mask (the workspace then holds the list of the keys that count), else 0.
  * VC_ERR_UNSUPPORTED for a value outside these. */

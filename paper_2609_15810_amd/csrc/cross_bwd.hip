@@ -47,7 +47,7 @@ __device__ __forceinline__ u4 pack_half(const v16f& s, int h) {
 // a second launch its part of dQ
 enum { WHOLE, PART_DELTA, PART_DQ };
 
-// GATHER: addresses per key (the keys are those of a list, or their stride is too far for one buffer)
+// GATHER: addresses per key (the keys are those of a list, or off_buffer)
 template <int DT, int D, bool GATHER, int MODE>
 __global__ __launch_bounds__(64 * NW, 2) void cross_dq(CrossArgs a) {
   using T = Tile<D>;
@@ -224,7 +224,7 @@ __global__ __launch_bounds__(64 * NW, 2) void cross_dq(CrossArgs a) {
 // so that two waves fit a SIMD, of two workgroups that are not in step: one's products and the other's vector work overlap.
 // (One wave a SIMD with V in registers: the products then leave their results in accumulation registers, 32 to 96 copies a
 // step; 283 us for 12 heads of 32760 rows and 512 keys.)
-// FAR: addresses per row (the rows' stride is too far for one buffer); SPLIT: leave parts
+// FAR: addresses per row (off_buffer); SPLIT: leave parts
 template <int DT, int D, bool FAR, bool SPLIT>
 __global__ __launch_bounds__(64 * NW, 2) void cross_dkv(CrossArgs a) {
   using T = Tile<D>;
@@ -440,8 +440,8 @@ hipError_t backward(const CrossArgs& a, hipStream_t s) {
   const int64_t heads = (int64_t)a.B * a.Hk;
   const unsigned gq = (unsigned)((int64_t)(a.R + QR - 1) / QR * heads * a.splits);
   const unsigned gk = (unsigned)((int64_t)(a.N + KB - 1) / KB * heads * a.row_splits);
-  const bool gather = a.idx || a.K.sn >= FAR_STRIDE || a.V.sn >= FAR_STRIDE;
-  const bool far = a.Q.sn >= FAR_STRIDE || a.dO.sn >= FAR_STRIDE;
+  const bool gather = a.idx || off_buffer(a.K, D) || off_buffer(a.V, D);
+  const bool far = off_buffer(a.Q, D) || off_buffer(a.dO, D);
   hipError_t e;
   if (a.splits > 1) {
     if (gather) cross_dq<DT, D, true, PART_DELTA><<<gq, 64 * NW, 0, s>>>(a);

@@ -159,6 +159,9 @@ __device__ __forceinline__ void mask_scores(v16f (&s)[2], int valid, int kh) {
 // through a buffer descriptor: a lane's offset from the tile's first row is the same for all tiles, and rows behind
 // the `valid` first are out of the buffer's range, which reads as zero without an access.
 constexpr int64_t FAR_STRIDE = 1 << 22;   // 256 rows of less than this stay below 2^31 bytes
+// Strides that a buffer does not serve: too far, or rows that overlap (shared ones: 0), of which those behind the last
+// would not be out of range
+inline bool off_buffer(const Strided& t, int d) { return t.sn >= FAR_STRIDE || t.sn < d; }
 template <int D, int ROWS, int NW>
 struct Copier {
   using T = Tile<D>;

@@ -35,8 +35,11 @@ constexpr int KT = 64;          // keys of a tile
 
 // A row's exponents are relative to a reference that follows its running maximum at a distance of at most LAG (log2
 // units): it moves, and the sums are rescaled, only where the maximum has left it by more. Probabilities then reach 2^LAG,
-// which the 16-bit types and the fp32 sums hold with the same relative errors.
+// which the 16-bit types and the fp32 sums hold with the same relative errors. In fp16 the reference starts SHIFT below the
+// maximum, so that probabilities reach 2^15 and those down to 2^-21 of the largest are normal numbers.
 constexpr float LAG = 8.f;
+template <int DT>
+constexpr float SHIFT = DT == VC_FP16 ? 7.f : 0.f;
 
 // A lane's row: O = o / l and lse
 template <int DT, int D>
@@ -50,7 +53,7 @@ __device__ __forceinline__ void finish_row(const CrossArgs& a, int b, int hk, in
   store_row<DT, D>(o, inv, row < a.R ? a.O.p + b * a.O.sb + w.h * a.O.sh + w.i * a.O.sn : nullptr, lane);
 }
 
-// GATHER: addresses per key (the keys are those of a list, or their stride is too far for one buffer);
+// GATHER: addresses per key (the keys are those of a list, or off_buffer);
 // SPLIT: leave parts
 template <int DT, int D, bool GATHER, bool SPLIT>
 __global__ __launch_bounds__(64 * NW, 2) void cross_fwd(CrossArgs a) {
@@ -147,8 +150,8 @@ __global__ __launch_bounds__(64 * NW, 2) void cross_fwd(CrossArgs a) {
 #pragma unroll
     for (int r = 1; r < 16; ++r) top = fmaxf(fmaxf(top, s[0][r]), s[1][r]);
     top = half_max(top) * a.c;
-    if (__builtin_amdgcn_ballot_w64(top > m + LAG)) {
-      const float up = top > m + LAG ? top : m, alpha = __builtin_amdgcn_exp2f(m - (up == -INFINITY ? 0.f : up));
+    if (__builtin_amdgcn_ballot_w64(top > m + (LAG + SHIFT<DT>))) {
+      const float up = top > m + (LAG + SHIFT<DT>) ? top - SHIFT<DT> : m, alpha = __builtin_amdgcn_exp2f(m - (up == -INFINITY ? 0.f : up));
       m = up;
       l *= alpha;
 #pragma unroll
@@ -324,8 +327,8 @@ __global__ __launch_bounds__(64 * WW, 2) void cross_fwd_wide(CrossArgs a, int to
 #pragma unroll
       for (int r = 1; r < 16; ++r) top = fmaxf(fmaxf(top, s[0][r]), s[1][r]);
       top = half_max(top) * a.c;
-      if (first || __builtin_amdgcn_ballot_w64(top > m + LAG)) {   // (the first tile of a block always clears its sums)
-        const float up = top > m + LAG ? top : m, alpha = __builtin_amdgcn_exp2f(m - (up == -INFINITY ? 0.f : up));
+      if (first || __builtin_amdgcn_ballot_w64(top > m + (LAG + SHIFT<DT>))) {   // (the first tile of a block always clears its sums)
+        const float up = top > m + (LAG + SHIFT<DT>) ? top - SHIFT<DT> : m, alpha = __builtin_amdgcn_exp2f(m - (up == -INFINITY ? 0.f : up));
         const bool anew = m == -INFINITY;   // (selected, not multiplied: what stands there may not be finite)
         m = up;
         l = anew ? 0.f : l * alpha;
@@ -485,7 +488,7 @@ __global__ __launch_bounds__(1024) void cross_keys(const uint8_t* mask, int64_t 
 template <int DT, int D>
 hipError_t forward(const CrossArgs& a, hipStream_t s) {
   const unsigned grid = (unsigned)((int64_t)(a.R + QR - 1) / QR * a.B * a.Hk * a.splits);
-  const bool gather = a.idx || a.K.sn >= FAR_STRIDE || a.V.sn >= FAR_STRIDE;
+  const bool gather = a.idx || off_buffer(a.K, D) || off_buffer(a.V, D);
   const int wide = (int)((int64_t)(a.M + WR - 1) / WR * a.B * a.Hq);
   if (a.splits == 1 && wide >= 256 && a.M >= WR && a.Q.sn < FAR_STRIDE && a.O.sn < FAR_STRIDE) {
     if (gather) cross_fwd_wide<DT, D, true><<<256, 64 * WW, 0, s>>>(a, wide);

@@ -52,7 +52,7 @@ BAD = vc.View(None, 0, 0, 0)
 @pytest.mark.parametrize("kw", [dict(B=0), dict(Hq=0), dict(Hk=0), dict(M=0), dict(N=0), dict(d=96), dict(d=32),
                                 dict(Hq=3), dict(B=1 << 20, M=1 << 10), dict(B=1 << 20, N=1 << 10),
                                 dict(Hk=1, B=1, M=(1 << 28) + 1), dict(Hq=1, Hk=1, B=1, N=(1 << 30) + 1),
-                                dict(B=1 << 23, M=1, N=1)])
+                                dict(B=1 << 23, M=1, N=1), dict(B=1 << 22, Hq=1, Hk=1, M=1, N=1)])
 def test_shapes_refused(L, kw):
     s = shape(**kw)
     assert forward(L, s, opts()) == 2 and backward(L, s, opts()) == 2

@@ -322,3 +322,39 @@ def test_wrong_tensors_refused():
     op = vc.CrossAttention(1, 4, 2, 33, 20, masked=True)
     with pytest.raises(vc.VcError):
         op.forward(p.Q, p.K, p.V, out)   # masked, without a mask
+
+
+@pytest.mark.parametrize("H,M", [(2, 40), (256, 300)])
+@pytest.mark.parametrize("N,shared", [(1, False), (70, True)])
+def test_infinite_value_of_few_or_shared_keys(H, M, N, shared):
+    # one key, or one row for all keys (stride 0): nothing behind the last key is taken for another
+    p = Problem(1, H, H, M, N)
+    p.V[:, :, 0, 9] = float("inf")
+    if shared:
+        p.V = p.V[:, :, :1].expand(1, H, N, 128)
+    out, _ = p.forward()
+    assert (out[..., 9] == float("inf")).all()
+    keep = torch.arange(128, device="cuda") != 9
+    assert out[..., keep].isfinite().all()
+    if shared or N == 1:   # every value is the one row: O is off by the roundings of P (half a step) and of O
+        v = p.V[:, :, :1, keep].double()
+        assert ((out[..., keep].double() - v).abs() <= 2.02 * 2.0 ** -8 * v.abs()).all()
+
+
+def test_small_probabilities_in_fp16():
+    """4095 keys at 2^-23.6 of one key with values of 0: their share of O is in probabilities far below fp16's normal range
+    of numbers up to 1. Scores are exact (one product); a probability is rounded in steps of 2^-31 of the largest or finer."""
+    N, d = 4096, 64
+    for H, M in ((1, 40), (256, 260)):
+        q = torch.zeros((1, H, M, d), dtype=FP, device="cuda")
+        k = torch.zeros((1, H, N, d), dtype=FP, device="cuda")
+        v = torch.ones_like(k)
+        q[..., 0], k[:, :, 1:, 0], v[:, :, 0] = 1.0, -23.6, 0.0
+        o = torch.empty_like(q)
+        vc.CrossAttention(1, H, H, M, N, d, dtype=FP, sm_scale=0.6931471805599453).forward(q, k, v, o)
+        x = float(k[0, 0, 1, 0].double())
+        small = 2.0 ** x
+        want = 4095 * small / (1 + 4095 * small)
+        # scale * log2(e) is 1 within 2^-23, times 23.6: a relative error of 2^-18; fp32 sums of 4096 terms: 2^-12
+        err = 2.0 ** -11 * want + 4095 * 2.0 ** -32 + (2.0 ** -18 + 2.0 ** -12) * want
+        assert float((o.double() - want).abs().max()) <= err
