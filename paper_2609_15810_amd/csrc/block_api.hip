@@ -147,7 +147,7 @@ size_t cross_args(const vc_cross_shape* s, const vc_cross_opts* o, bool backward
   }
   if (a.splits > 1) {
     a.part_o = reinterpret_cast<float*>(part(a.splits * rows * a.d * 4));
-    a.part_ml = reinterpret_cast<float*>(part(a.splits * rows * (backward ? 4 : 8)));
+    a.part_ml = reinterpret_cast<float*>(part(a.splits * rows * 8));
   }
   if (backward) {
     a.stats = reinterpret_cast<float*>(part((size_t)a.B * a.Hq * vc::cross_stat_rows(a.M) * 8));

@@ -1,6 +1,6 @@
 // Gradients of the attention to the states of another sequence (cross_fwd.hip), from lse and O of the forward pass:
 //
-//   P = exp(c' Q K^T - lse),  dV = P^T dO,  dP = dO V^T,  delta_i = sum_j P_ij dP_ij,
+//   P = exp(c' Q K^T - lse),  dV = P^T dO,  dP = dO V^T,  delta_i = sum_j P_ij dP_ij / sum_j P_ij,
 //   dS = P (dP - delta),  dQ = c' dS K,  dK = c' dS^T Q,
 //
 // with dK and dV summed over the query heads of a key head. Two kernels form S and dP each, so that every sum is
@@ -14,10 +14,15 @@
 // order for the next product, whose other operand is read from LDS by transposing reads. P and dS are rounded to the
 // operands' 16 bits, as the matrix instructions take them; sums are fp32.
 //
-// delta is formed from P and dP, in a first walk over the keys. It equals sum_c dO_ic O_ic, which costs no walk, but O comes
-// rounded to 16 bits, and an error of delta does not average out: dS of a row is off by P times it. Measured on 12 heads of
-// 32760 rows and 512 keys in bf16, rms errors of dQ / dK relative to their size, and the time of the gradients: from O 0.0038 /
-// 0.0030, 405 us; from P and dP 0.0024 / 0.0024 (a rounding of dQ itself: 0.0017). With one key, dS is exactly 0.
+// Two things cost matrix products for the sake of dQ and dK. delta is formed from P and dP, in a first walk over the keys. It
+// equals sum_c dO_ic O_ic, which costs no walk, but O comes rounded to 16 bits, and an error of delta does not average out: dS
+// of a row is off by P times it. (The sum of P is 1 but for the error of lse, which dS then does not see.) And for dQ, dS is
+// taken as two 16-bit numbers: the dS of a row add up to 0, which takes out of dQ what all keys have in common, but their
+// roundings do not, and keys tend to have large means. Measured on 12 heads of 32760 rows and 512 keys in bf16, rms errors of dQ
+// and dK relative to their size (a rounding of them alone: 0.0017) and the time of cross_dq:
+//   delta from O                          0.0038, 0.0030   190 us
+//   delta from P and dP                   0.0025, 0.0024   261 us
+//   and dS in two numbers for dQ          0.0017, 0.0023   310 us
 #include <type_traits>
 
 #include "cross_common.hpp"
@@ -42,6 +47,32 @@ __device__ __forceinline__ u4 pack_half(const v16f& s, int h) {
   for (int i = 0; i < 4; ++i) r[i] = pack2<DT>(s[8 * h + 2 * i], s[8 * h + 2 * i + 1]);
   return r;
 }
+// what that rounded off
+template <int DT>
+__device__ __forceinline__ u4 pack_rest(const v16f& s, int h, const u4& rounded) {
+  u4 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t w = rounded[i];
+    float x, y;
+    if constexpr (DT == VC_BF16) {
+      x = bf16_lo(w), y = bf16_hi(w);
+    } else {
+      typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+      const h2 f = __builtin_bit_cast(h2, w);
+      x = f[0], y = f[1];
+    }
+    r[i] = pack2<DT>(s[8 * h + 2 * i] - x, s[8 * h + 2 * i + 1] - y);
+  }
+  return r;
+}
+
+// In cross_dkv probabilities are 2^shift times themselves: fp16's normal range ends at 2^-14, which the probabilities of
+// many keys fall below
+template <int DT>
+constexpr float P_SHIFT = DT == VC_FP16 ? 15.f : 0.f;
+template <int DT>
+constexpr float P_UNIT = DT == VC_FP16 ? 1.f / 32768.f : 1.f;
 
 // What a launch of cross_dq forms: delta and dQ in two walks over all keys; or over a part of the keys its part of delta, and in
 // a second launch its part of dQ
@@ -117,9 +148,12 @@ __global__ __launch_bounds__(64 * NW, 2) void cross_dq(CrossArgs a) {
   }
   const float l2 = a.lse[((size_t)b * a.Hq + qr.h) * a.M + qr.i] * 1.4426950408889634f;
   const size_t heads = (size_t)a.B * a.Hk;
-  float delta = 0.f;   // in the first walk, the sum of this lane's keys
+  float delta = 0.f, sum = 0.f;   // sums of P dP and of P over the keys; then delta
   if (MODE == PART_DQ && row < a.R)
-    for (int s = 0; s < a.splits; ++s) delta += a.part_ml[(s * heads + bh) * a.R + row];
+    for (int s = 0; s < a.splits; ++s) {
+      const float2 x = *reinterpret_cast<const float2*>(a.part_ml + 2 * ((s * heads + bh) * a.R + row));
+      delta += x.x, sum += x.y;
+    }
   const RowOperands<D> rows0(lane);
   const ColOperands<D> cols0(lane);
   v16f acc[DB];
@@ -155,6 +189,7 @@ __global__ __launch_bounds__(64 * NW, 2) void cross_dq(CrossArgs a) {
   };
   int u = 0;
   if (MODE != PART_DQ) {
+    float part[8] = {};   // in four chains each: the operations of one wait for each other
     for (; u < tiles; ++u) {
       arrive(u);
       if (!active) continue;
@@ -163,45 +198,54 @@ __global__ __launch_bounds__(64 * NW, 2) void cross_dq(CrossArgs a) {
         v16f s, dp;
         products((u & 1) * TB, x, k1 - k0 - u * KT, s, dp);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) delta = __builtin_fmaf(s[r], dp[r], delta);
+        for (int r = 0; r < 16; ++r) {
+          part[r & 3] = __builtin_fmaf(s[r], dp[r], part[r & 3]);
+          part[4 + (r & 3)] += s[r];
+        }
       }
     }
-    delta = half_sum(delta);
-  }
-  if (MODE != PART_DELTA) {
-    for (int t = 0; t < tiles; ++t, ++u) {
-      arrive(u);
-      if (!active) continue;
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        v16f s, dp;
-        products((u & 1) * TB, x, k1 - k0 - t * KT, s, dp);
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] *= dp[r] - delta;
-        const u4 ds[2] = {pack_half<DT>(s, 0), pack_half<DT>(s, 1)};
-        __builtin_amdgcn_sched_barrier(0);
-        const ColOperands<D> cols = cols0.move(lds_addr(kt[0]) + (u & 1) * TB);
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int db = 0; db < DB; ++db) acc[db] = mma<DT>(cols.get((32 * x + 16 * h) * T::ROW, db), ds[h], acc[db]);
-        issue_reads<8>();
-        issue_products<2 * DB - 4, 2>();
-        issue_products<4, 0>();
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    }
+    delta = half_sum((part[0] + part[1]) + (part[2] + part[3]));
+    sum = half_sum((part[4] + part[5]) + (part[6] + part[7]));
   }
   if (MODE == PART_DELTA) {
-    if (row < a.R && kh == 0) a.part_ml[(split * heads + bh) * a.R + row] = delta;
+    if (row < a.R && kh == 0)
+      *reinterpret_cast<float2*>(a.part_ml + 2 * ((split * heads + bh) * a.R + row)) = make_float2(delta, sum);
     return;
+  }
+  delta = sum > 0.f ? delta / sum : 0.f;
+  for (int t = 0; t < tiles; ++t, ++u) {
+    arrive(u);
+    if (!active) continue;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      v16f s, dp;
+      products((u & 1) * TB, x, k1 - k0 - t * KT, s, dp);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] *= dp[r] - delta;
+      const u4 ds[2] = {pack_half<DT>(s, 0), pack_half<DT>(s, 1)};
+      const u4 rest[2] = {pack_rest<DT>(s, 0, ds[0]), pack_rest<DT>(s, 1, ds[1])};
+      __builtin_amdgcn_sched_barrier(0);
+      const ColOperands<D> cols = cols0.move(lds_addr(kt[0]) + (u & 1) * TB);
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+          const u4 k = cols.get((32 * x + 16 * h) * T::ROW, db);
+          acc[db] = mma<DT>(k, ds[h], acc[db]);
+          acc[db] = mma<DT>(k, rest[h], acc[db]);
+        }
+      issue_reads<8>();
+      issue_products<4 * DB - 8, 1>();
+      issue_products<8, 0>();
+      __builtin_amdgcn_sched_barrier(0);
+    }
   }
 
   // what cross_dkv needs of a row; the rows that fill a head's last tile get probabilities of 0
   if (split == 0 && kh == 0 && row < a.R) {
     const int fill = stat_rows(a.M);
     float* st = a.stats + 2 * (((size_t)b * a.Hq + qr.h) * fill + qr.i);
-    *reinterpret_cast<float2*>(st) = make_float2(l2, delta);
+    *reinterpret_cast<float2*>(st) = make_float2(l2 - P_SHIFT<DT>, delta * P_UNIT<DT>);
     if (qr.i == a.M - 1)
       for (int i = 1; i < fill - qr.i; ++i) *reinterpret_cast<float2*>(st + 2 * i) = make_float2(INFINITY, 0.f);
   }
@@ -323,7 +367,7 @@ __global__ __launch_bounds__(64 * NW, 2) void cross_dkv(CrossArgs a) {
       for (int e = 0; e < 4; ++e) {
         const int r = 4 * g + e;
         s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], a.c, -l2[e]));
-        dp[r] = s[r] * (dp[r] - dl[e]);
+        dp[r] = s[r] * __builtin_fmaf(dp[r], P_UNIT<DT>, -dl[e]);
       }
     }
     u4 p[2], ds[2];
@@ -373,7 +417,7 @@ __global__ __launch_bounds__(64 * NW, 2) void cross_dkv(CrossArgs a) {
     return j < a.N ? t.p + b * t.sb + hk * t.sh + key * t.sn : nullptr;
   };
   store_row<DT, D>(dk, a.scale, row_of(a.dK), lane);
-  store_row<DT, D>(dv, 1.f, row_of(a.dV), lane);
+  store_row<DT, D>(dv, P_UNIT<DT>, row_of(a.dV), lane);
 }
 
 // Sums of parts [part][row][D] at p (rows * D apart by `step`): as cross_join, d / 4 lanes and `groups` of them a row;
@@ -426,7 +470,7 @@ __global__ __launch_bounds__(256) void cross_join_dkv(CrossArgs a, int groups) {
   const float4 o = join_parts<D>(a.part_kv + (which * keys + at) * D, 2 * keys * D, a.row_splits, groups,
                                  in && j < keys_of(a, b));
   if ((slot & (groups - 1)) != 0 || !in) return;
-  const float f = which ? 1.f : a.scale;
+  const float f = which ? P_UNIT<DT> : a.scale;
   const Strided& t = which ? a.dV : a.dK;
   const int64_t i = a.idx ? a.idx[(size_t)b * a.N + j] : j;
   *reinterpret_cast<u2*>(t.p + b * t.sb + hk * t.sh + i * t.sn + c) =

@@ -122,7 +122,7 @@ struct CrossArgs {
   // keys split over workgroups: `splits` parts of `chunk` keys, joined from
   int splits, chunk;
   float* part_o;         // [splits][B Hk][R][d] unnormalised outputs (backward: parts of dQ)
-  float* part_ml;        // [splits][B Hk][R][2] running maximum (log2 units) and sum (backward: [splits][B Hk][R] of delta)
+  float* part_ml;        // [splits][B Hk][R][2] running maximum (log2 units) and sum (backward: sums of P dP and of P)
   // backward
   float* stats;          // [B][Hq][cross_stat_rows(M)][2] lse in log2 units and delta
   int row_splits, row_chunk;   // row tiles split over workgroups that form dK and dV

@@ -121,6 +121,9 @@ class Cross:
         add = 1 + (rows + N) * 2.0 ** -24   # fp32 sums over rows or keys, of terms of these sizes
         self.dV_err = out(self.dV, add * group((half + rel) * Pt @ G.abs()) + (rows * 2.0 ** -24) * group(Pt @ G.abs()) +
                           tiny * group(G.abs().sum(2, keepdim=True).expand(B, Hq, N, d)))
+        # as dV_err, of probabilities in fp16 that are rounded as 2^15 times themselves
+        self.dV_fine = out(self.dV, add * group((half + rel) * Pt @ G.abs()) + (rows * 2.0 ** -24) * group(Pt @ G.abs()) +
+                           tiny * 2.0 ** -15 * group(G.abs().sum(2, keepdim=True).expand(B, Hq, N, d)))
         sizeS = dS.abs()
         self.dQ_err = out(self.dQ, scale * (add * (dSerr @ Kg.abs()) + N * 2.0 ** -24 * (sizeS @ Kg.abs()) +
                                             tiny * Kg.abs().sum(2, keepdim=True)))

@@ -358,3 +358,45 @@ def test_small_probabilities_in_fp16():
         # scale * log2(e) is 1 within 2^-23, times 23.6: a relative error of 2^-18; fp32 sums of 4096 terms: 2^-12
         err = 2.0 ** -11 * want + 4095 * 2.0 ** -32 + (2.0 ** -18 + 2.0 ** -12) * want
         assert float((o.double() - want).abs().max()) <= err
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("B,H,M,N,d", [(1, 2, 150, 200, 128), (2, 2, 40, 77, 64), (1, 1, 16, 2500, 128)])
+def test_keys_with_a_common_part(dtype, B, H, M, N, d):
+    """Keys of large channel means, which the dS of a row cancel. dQ is rounded by at most half a step, so that this alone
+    leaves an rms error of half a step of its rms; a tenth of that is left for the sums in fp32. (Roundings of dS, 0.4 of half a
+    step in rms, times means of 8 times the keys' spread would leave 3.5 of it.)"""
+    p = Problem(B, H, H, M, N, d, dtype, gain=0.2)
+    shift = (10.0 * torch.randn((1, H, 1, d), generator=torch.Generator().manual_seed(9))).to(dtype)
+    p.cpu[1] = p.cpu[1] + shift
+    p.K = p.cpu[1].cuda()
+    q, k, v, do = p.cpu
+    ref = O.Cross(q, k, v, p.valid, dtype, 0.0, do)
+    dQ = p.backward(*p.forward())[0].cpu().double()
+    near(dQ, ref.dQ, ref.dQ_err, "dQ")
+    rms = lambda t: float(t.square().mean().sqrt())  # noqa: E731
+    assert rms(dQ - ref.dQ) <= 1.1 * O.HALF[dtype] * rms(ref.dQ)
+
+
+@pytest.mark.parametrize("M", [40, 300])
+def test_gradients_of_many_keys_in_fp16(M):
+    # probabilities of 1 / 20000, below fp16's normal numbers
+    p = Problem(1, 1, 1, M, 20000, 64, FP, gain=0.3)
+    q, k, v, do = p.cpu
+    ref = O.Cross(q, k, v, p.valid, FP, 0.0, do)
+    dV = p.backward(*p.forward())[2]
+    near(dV, ref.dV, ref.dV_fine, "dV")
+    small = ref.dV.abs().square().mean().sqrt()
+    assert float((dV.cpu().double() - ref.dV).square().mean().sqrt() / small) < 2.0 ** -11   # two roundings' rms is 0.7 of it
+
+
+@pytest.mark.parametrize("M,scale", [(150, 0.0), (40, 40.0)])
+def test_one_key_has_no_gradient_of_scores(M, scale):
+    """dS of a single key is 0: what is left of dP is its fp32 sums' roundings (d + 8 of 2^-24 of its terms' sizes), not the
+    error of lse (2^-24 of the scores, of several thousand), which P and with it delta's terms carry"""
+    p = Problem(1, 2, 2, M, 1, scale=scale, gain=10.0)
+    dQ, dK, _ = (t.cpu().double() for t in p.backward(*p.forward()))
+    q, k, v, do = (t.double() for t in p.cpu)
+    left = 136 * 2.0 ** -24 * (do.abs() @ v.abs().transpose(2, 3)) * (scale or 128 ** -0.5)
+    assert (dQ.abs() <= left * k.abs()).all()
+    assert (dK.abs() <= (left * q.abs()).sum(2, keepdim=True)).all()
