@@ -396,9 +396,9 @@ typedef struct {
 /* Options of the attention to another sequence.
  *   dtype    : VC_BF16 or VC_FP16, of all tensors. The products take 16-bit operands: the probabilities (and in the
  *              backward pass their gradients) are rounded to dtype before they enter a product. Sums and the softmax's
- *              statistics are fp32, outputs are rounded once. With VC_FP16, probabilities of the backward pass and
- *              gradients of scores (dS, of the size of dO times V) have fp16's range: in steps of 2^-24 at the
- *              least, and dS below 65520, where a loss scaled as for any fp16 training keeps it.
+ *              statistics are fp32, outputs are rounded once. With VC_FP16, gradients of scores (dS,
+ *              of the size of dO times V) have fp16's range: steps of 2^-24 at the least, and below 65520, where a loss
+ *              scaled as for any fp16 training keeps them.
  *   sm_scale : score scale, >= 0 with sm_scale * log2(e) finite in fp32; 0 selects 1/sqrt(d).
  *   masked   : 1 = the calls give a k_mask (the workspace then holds the list of the keys that count), else 0.
  * VC_ERR_UNSUPPORTED for a value outside these. */

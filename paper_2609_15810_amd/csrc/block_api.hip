@@ -108,7 +108,7 @@ vc_status check_cross(const vc_cross_shape* s, const vc_cross_opts* o) {
     return VC_ERR_SHAPE;
   const int64_t rows = (int64_t)(s->Hq / s->Hk) * s->M, heads = (int64_t)s->B * s->Hk;
   if (rows > (1 << 30) || s->N > (1 << 30)) return VC_ERR_SHAPE;
-  // workgroups of 128 rows or keys, or of 1024 threads a batch item: a launch has fewer than 2^32 threads
+  // workgroups of 128 rows or keys, or of 1024 threads for 4096 keys of an item: a launch has fewer than 2^32 threads
   if (s->B >= (1 << 22) || (rows + 127) / 128 * heads >= (1 << 24) || ((int64_t)s->N + 127) / 128 * heads >= (1 << 24)) return VC_ERR_SHAPE;
   if (o->dtype != VC_BF16 && o->dtype != VC_FP16) return VC_ERR_UNSUPPORTED;
   if (!(o->sm_scale >= 0.f) || !std::isfinite(o->sm_scale * 1.4426950408889634f)) return VC_ERR_UNSUPPORTED;

@@ -1,4 +1,4 @@
-// Gradients of the attention to the states of another sequence (cross_fwd.hip), from lse and O of the forward pass:
+// Gradients of the attention to the states of another sequence (cross_fwd.hip), from lse of the forward pass:
 //
 //   P = exp(c' Q K^T - lse),  dV = P^T dO,  dP = dO V^T,  delta_i = sum_j P_ij dP_ij / sum_j P_ij,
 //   dS = P (dP - delta),  dQ = c' dS K,  dK = c' dS^T Q,

@@ -400,3 +400,26 @@ def test_one_key_has_no_gradient_of_scores(M, scale):
     left = 136 * 2.0 ** -24 * (do.abs() @ v.abs().transpose(2, 3)) * (scale or 128 ** -0.5)
     assert (dQ.abs() <= left * k.abs()).all()
     assert (dK.abs() <= (left * q.abs()).sum(2, keepdim=True)).all()
+
+
+@pytest.mark.parametrize("N", [1023, 4096, 4097, 16400, 40001])
+def test_lists_of_many_keys(N):
+    """masks of more keys than a pass over them takes, rows of the mask at odd addresses, an item of which no key counts and
+    one of which all do: O of the masked keys is that of the keys that are left, to the order of the sums"""
+    g = torch.Generator().manual_seed(N)
+    rand = lambda *s: torch.randn(s, generator=g).to(BF).cuda()  # noqa: E731
+    B, H, M, d = 4, 1, 3, 64
+    Q, K, V = rand(B, H, M, d), rand(B, H, N, d), rand(B, H, N, d)
+    mask = (torch.rand((B, N), generator=g) < 0.5)
+    mask[1], mask[2] = True, False
+    wide = torch.zeros((B, N + 3), dtype=torch.bool, device="cuda")
+    wide[:, 1:N + 1] = mask.cuda()
+    k_len = torch.tensor([N, N, N, N // 2], dtype=torch.int32)
+    out, lse = torch.empty_like(Q), torch.empty((B, H, M), device="cuda")
+    vc.CrossAttention(B, H, H, M, N, d, masked=True).forward(Q, K, V, out, lse, k_len=k_len.cuda(), k_mask=wide[:, 1:N + 1])
+    mask &= torch.arange(N)[None] < k_len[:, None]
+    ref = O.Cross(Q.cpu(), K.cpu(), V.cpu(), mask, BF)
+    near(out, ref.O, ref.O_err, "O")
+    assert (out[2] == 0).all() and (lse[2] == -float("inf")).all()
+    keep = torch.tensor([0, 1, 3])
+    assert ((lse.cpu().double() - ref.lse)[keep].abs() <= ref.lse_err[keep].expand(3, H, M)).all()
