@@ -187,6 +187,7 @@ __global__ __launch_bounds__(64 * NW, 2) void cross_dq(CrossArgs a) {
       fetch(u + 2);
     }
   };
+  // (The second half of a tile without keys is left out: 40 heads of 75600 rows over 77 keys, all gradients, 1176 -> 1105 us.)
   int u = 0;
   if (MODE != PART_DQ) {
     float part[8] = {};   // in four chains each: the operations of one wait for each other
@@ -195,6 +196,7 @@ __global__ __launch_bounds__(64 * NW, 2) void cross_dq(CrossArgs a) {
       if (!active) continue;
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
+        if (k1 - k0 - u * KT <= 32 * x) break;
         v16f s, dp;
         products((u & 1) * TB, x, k1 - k0 - u * KT, s, dp);
 #pragma unroll
@@ -218,6 +220,7 @@ __global__ __launch_bounds__(64 * NW, 2) void cross_dq(CrossArgs a) {
     if (!active) continue;
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
+      if (k1 - k0 - t * KT <= 32 * x) break;
       v16f s, dp;
       products((u & 1) * TB, x, k1 - k0 - t * KT, s, dp);
 #pragma unroll

@@ -10,10 +10,11 @@
 // tile ahead.
 //
 // The rows of a key head are those of all its query heads, one head behind the other, so that grouped heads share
-// tiles and a token's few queries share one. Calls with rows for 256 workgroups of 256 take cross_fwd_wide instead, whose
-// workgroups walk over blocks of rows of a head. Measured (us, this kernel / wide): 12 heads of 32760 rows over 512 keys 129 /
-// 122, over 1024 keys 232 / 214; 40 heads of 75600 rows over 512 keys 1099 / 1036 (1.5 GB, 793 GFLOP); with 192 workgroups
-// (12 heads of 4096 rows) 26 / 26, below that it loses CUs.
+// tiles and a token's few queries share one. Calls of 128 channels with rows for 256 workgroups of 256 take cross_fwd_wide
+// instead, whose workgroups walk over blocks of rows of a head. Measured (us, this kernel / wide): 12 heads of 32760 rows over
+// 64 keys 44 / 42, over 512 keys 129 / 122, over 1024 keys 232 / 214; 40 heads of 75600 rows over 512 keys 1099 / 1036 (1.5 GB,
+// 793 GFLOP); with 192 workgroups (12 heads of 4096 rows) 26 / 26, below that it loses CUs. Of 64 channels, four waves of this
+// kernel fit a SIMD, and the wide one has two: 12 heads of 32760 rows over 64 keys 23 / 28, over 512 66 / 88, over 2048 222 / 291.
 //
 // What bounds it: 16 bytes of LDS are read per product and lane, exponentials and products take about the same time, and the
 // card lowers its clock under the matrix cores' load (1.7 GHz at their full rate on random operands); the sustained rate of
@@ -514,10 +515,13 @@ hipError_t forward(const CrossArgs& a, hipStream_t s) {
   const unsigned grid = (unsigned)((int64_t)(a.R + QR - 1) / QR * a.B * a.Hk * a.splits);
   const bool gather = a.idx || off_buffer(a.K, D) || off_buffer(a.V, D);
   const int wide = (int)((int64_t)(a.M + WR - 1) / WR * a.B * a.Hq);
-  if (a.splits == 1 && wide >= 256 && a.M >= WR && a.Q.sn < FAR_STRIDE && a.O.sn < FAR_STRIDE) {
-    if (gather) cross_fwd_wide<DT, D, true><<<256, 64 * WW, 0, s>>>(a, wide);
-    else cross_fwd_wide<DT, D, false><<<256, 64 * WW, 0, s>>>(a, wide);
-  } else if (a.splits > 1) {
+  if constexpr (D == 128)
+    if (a.splits == 1 && wide >= 256 && a.M >= WR && a.Q.sn < FAR_STRIDE && a.O.sn < FAR_STRIDE) {
+      if (gather) cross_fwd_wide<DT, D, true><<<256, 64 * WW, 0, s>>>(a, wide);
+      else cross_fwd_wide<DT, D, false><<<256, 64 * WW, 0, s>>>(a, wide);
+      return hipGetLastError();
+    }
+  if (a.splits > 1) {
     if (gather) cross_fwd<DT, D, true, true><<<grid, 64 * NW, 0, s>>>(a);
     else cross_fwd<DT, D, false, true><<<grid, 64 * NW, 0, s>>>(a);
     const hipError_t e = hipGetLastError();
