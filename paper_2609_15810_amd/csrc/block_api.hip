@@ -271,7 +271,7 @@ size_t vc_norm_rope_workspace_size(const vc_norm_rope_shape* shape, const vc_nor
   if (check_norm_rope(shape, opts) != VC_OK) return (size_t)-1;
   if (opts->norm == VC_NORM_NONE) return 0;
   const size_t C = norm_weights(opts, shape->Hq, shape->d) + (shape->Hk ? norm_weights(opts, shape->Hk, shape->d) : 0);
-  return C * 4 * vc::norm_rope_parts((int64_t)shape->B * shape->N);
+  return C * 4 * vc::norm_rope_parts((int64_t)shape->B * shape->N, shape->Hk ? 2 : 1);
 }
 
 vc_status vc_norm_rope_backward(const vc_norm_rope_shape* shape, const vc_norm_rope_opts* opts, const vc_view* q,
@@ -315,7 +315,7 @@ vc_status vc_norm_rope_backward(const vc_norm_rope_shape* shape, const vc_norm_r
     t.dw = dw[i];
     if (dw[i]) {
       t.dw_part = part;
-      part += (size_t)t.weights * vc::norm_rope_parts(a.tokens);
+      part += (size_t)t.weights * vc::norm_rope_parts(a.tokens, a.ntensors);
     }
   }
   if (!norm) {

@@ -567,10 +567,13 @@ int past_caches(const NormRopeArgs& a, int tensors) {
 
 }  // namespace
 
-int norm_rope_parts(int64_t tokens) {
-  // workgroups of the backward kernel, each of which leaves a row of partial weight sums
-  const int64_t w = (tokens + 4 * WAVES - 1) / (4 * WAVES);
-  return (int)(w < 1 ? 1 : (w > 512 ? 512 : w));
+int norm_rope_parts(int64_t tokens, int ntensors) {
+  // workgroups of the backward kernel, each of which leaves a row of partial weight sums: as many as fit the CUs at once, two
+  // each, and no more than have a token each. Measured (us, this / twice as many): 12 + 12 heads of 32760 tokens, norms per head
+  // 141 / 140, per token 148 / 156; of 16000 tokens 71 / 75, 74 / 84. With 16 tokens each instead of one, 40 + 40 heads of 16
+  // tokens take 28 instead of 13 per head and 52 instead of 14 per token.
+  const int64_t most = 512 / ntensors;
+  return (int)(tokens < most ? tokens : most);
 }
 
 hipError_t launch_norm_rope(NormRopeArgs a, hipStream_t s) {
@@ -582,7 +585,8 @@ hipError_t launch_norm_rope(NormRopeArgs a, hipStream_t s) {
     units += a.t[i].groups * r;
   }
   // heads of a slot that a wave has in flight: more of them for large calls; one, so that the heads of a token go to
-  // several waves, where there are few tokens
+  // several waves, where there are few tokens. Measured (us, the rotation alone, one / more): 40 heads of 16 tokens 3.9 / 4.5, of
+  // 256 tokens (2560 units) 5.1 / 5.4; 12 heads of 2000 tokens (8000 units) 8.5 / 7.8, of 16000 52 / 43
   const int nb = a.norm == VC_NORM_TOKEN ? (int)rounds : units <= 4096 ? 1 : rounds <= 2 ? (int)rounds : 4;
   int64_t grid = 1;
   for (int i = 0; i < a.ntensors; ++i) {
@@ -590,7 +594,9 @@ hipError_t launch_norm_rope(NormRopeArgs a, hipStream_t s) {
     const int64_t u = (int64_t)t.groups * ((t.H + nb * t.P - 1) / (nb * t.P)), teams = WAVES / t.W;
     grid = (u + teams - 1) / teams > grid ? (u + teams - 1) / teams : grid;
   }
-  const int64_t most = 2048 / a.ntensors;
+  // workgroups: half of them with 12 + 12 heads of 32760 tokens take 73 instead of 68 us for the rotation alone, 81 instead of 77
+  // with norms per token; twice as many 66 and 80, and 54 instead of 50 for 16000 tokens with these norms
+  const int64_t most = 4096 / a.ntensors;
   return dispatch<false>(a, nb, (int)(grid < most ? grid : most), 0, s);
 }
 
@@ -605,7 +611,7 @@ hipError_t launch_norm_rope_backward(NormRopeArgs a, hipStream_t s) {
     C = t.weights > C ? t.weights : C;
     weights = weights || t.dw_part;
   }
-  const int parts = norm_rope_parts(a.tokens);
+  const int parts = norm_rope_parts(a.tokens, a.ntensors);
   hipError_t e = dispatch<true>(a, nb, parts, (size_t)C * 4, s);
   if (e != hipSuccess || !weights) return e;
   norm_rope_join<<<dim3((unsigned)((C + 7) / 8), (unsigned)a.ntensors), 1024, 0, s>>>(a, parts);

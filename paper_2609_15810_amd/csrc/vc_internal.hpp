@@ -138,7 +138,7 @@ hipError_t launch_fp8_score_product(const uint8_t* a, const uint8_t* b, const fl
 
 hipError_t launch_norm_rope(NormRopeArgs a, hipStream_t s);
 hipError_t launch_norm_rope_backward(NormRopeArgs a, hipStream_t s);
-int norm_rope_parts(int64_t tokens);   // workgroups of the backward kernel
+int norm_rope_parts(int64_t tokens, int ntensors);   // workgroups of the backward kernel for each tensor
 
 // Which keys count, as a list: idx [B][N], count [B]
 hipError_t launch_cross_keys(const uint8_t* k_mask, int64_t stride, const int32_t* k_len, int B, int N, int32_t* idx,
