@@ -521,7 +521,8 @@ hipError_t backward(const CrossArgs& a, hipStream_t s) {
 void cross_plan_backward(CrossArgs& a) {
   using namespace cross;
   cross_plan(a);
-  // row tiles are split where the keys alone do not give every CU two workgroups
+  // Row tiles are split where the keys alone do not give every CU two workgroups, into as many parts as fit at once (12 heads of
+  // 32760 rows and 512 keys: 10 parts 218 us, one workgroup a CU 302, 21 parts 227)
   const int64_t base = (int64_t)(a.N + KB - 1) / KB * a.B * a.Hk, tiles = (int64_t)a.G * ((a.M + RT - 1) / RT);
   int64_t splits = base >= 256 ? 1 : 512 / base;
   if (splits > tiles) splits = tiles;
